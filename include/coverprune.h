@@ -20,6 +20,16 @@
  *   coverprune_lite_select CoverPrune-Lite: Morton ordering, capacity-guided
  *                          grouping and per-group prototypes (Sec. 4, Eq. 17-20).
  *
+ * and, for the language model that reads the kept tokens (Sec. 5.1: pruning
+ * comes immediately before its prefill), the operators of its serving layer:
+ *
+ *   coverprune_rms_norm    root-mean-square norm with the residual's addition,
+ *                          optionally rounded to 8 bits with row scales;
+ *   coverprune_w4_matvec   a few rows times 4-bit weights with group scales;
+ *   coverprune_kv_append   position rotation, and keys and values into a paged
+ *                          cache at the positions the tokens had in the video;
+ *   coverprune_paged_attention  one new token of each sequence over that cache.
+ *
  * Conventions shared by every entry point
  *   - Token j has a feature row f_j (D values), a 3D position x_j (metres) and
  *     the integer index tau_j of the frame it came from (problem setup, Sec. 3.2).
@@ -72,7 +82,9 @@ typedef enum {
   CP_ERR_HIP = 4          /* the HIP runtime reported an error while enqueuing */
 } cp_status;
 
-typedef enum { CP_F32 = 0, CP_BF16 = 1 } cp_dtype;
+/* CP_F16 and CP_E4M3 (8 bits: 3 after the leading one, exponents down to -6,
+ * largest 448, no infinity) are types of the serving operators. */
+typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_F16 = 2, CP_E4M3 = 3 } cp_dtype;
 
 /* Weights of Eq. 8.  lambda_* >= 0 weight the feature, spatial and temporal
  * terms; kappa >= 0 shapes phi_kappa(z) = log(1 + kappa z) / log(1 + kappa),
@@ -483,6 +495,113 @@ cp_status coverprune_lite_select(const void* feats, cp_dtype dtype, int64_t n, i
                                  int64_t k, cp_fst_weights w, float voxel_size, int32_t* selected,
                                  int32_t* group, double* objective, double* token_cost, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Serving operators: the decode step of the language model that receives the
+ * kept tokens.  They follow the conventions above, and
+ *   - a count of rows or tokens may be 0: nothing is enqueued then;
+ *   - every rounding is to nearest even; values beyond +-448 become +-448 in
+ *     CP_E4M3, NaN stays NaN;
+ *   - sums, softmax statistics and norms are held in float32.
+ */
+
+/* Root-mean-square norm.
+ *   h = x + residual (float32),  y_j = h_j weight_j / sqrt(mean_j h_j^2 + eps)
+ *
+ *   x         [rows, d], dtype CP_BF16, CP_F16 or CP_F32; 1 <= d <= 65536 (the
+ *             rows are read 16 bytes at a time when d % 8 == 0)
+ *   residual  [rows, d] dtype, or NULL: h = x
+ *   weight    [d] dtype
+ *   eps       finite, >= 0
+ *   out       [rows, d]: y rounded to dtype (out_dtype == dtype), or
+ *             (out_dtype == CP_E4M3) y_j / scale rounded, scale = max_j |y_j| / 448
+ *             (codes 0 where scale is 0)
+ *   out_scale [rows] float: the scales; required with CP_E4M3, unused otherwise
+ *   residual_out  [rows, d] dtype: h rounded; required with residual (which it
+ *             may be), unused otherwise
+ */
+cp_status coverprune_rms_norm(const void* x, cp_dtype dtype, int64_t rows, int64_t d, const void* residual,
+                              const void* weight, float eps, void* out, cp_dtype out_dtype, float* out_scale,
+                              void* residual_out, void* stream);
+
+/* A few rows times 4-bit weights with group scales.
+ *   y[i, o] = x_scale_i sum_j x[i, j] (code[o, j] - zero[o, j / group]) scale[o, j / group]
+ *
+ *   x        [m, k], x_dtype == dtype or CP_E4M3
+ *   x_scale  [m] float with CP_E4M3 (as coverprune_rms_norm writes them), NULL otherwise
+ *   weight   [n, k / 2] bytes, two 4-bit codes each, the even j in the low half
+ *   scale    [n, k / group] dtype
+ *   zero     [n, k / group] bytes, the code that stands for 0; NULL: 8
+ *   group    a multiple of 32 that divides k (k < 2^31)
+ *   dtype    CP_BF16 or CP_F16
+ *   y        [m, n], y_dtype == dtype or CP_F32
+ * The time is that of reading the weights up to m = 16; every further 64 rows
+ * read them again (from a cache, where they fit one).
+ */
+cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_scale, const uint8_t* weight,
+                               const void* scale, const uint8_t* zero, int64_t m, int64_t n, int64_t k, int64_t group,
+                               cp_dtype dtype, void* y, cp_dtype y_dtype, void* stream);
+
+/* Position rotation of queries and keys, and keys and values into a paged
+ * cache.  With angle = position * inv_freq_i for pair i of a head,
+ *   a' = magnitude (a cos - b sin),  b' = magnitude (b cos + a sin),
+ * where the pair is elements i and i + rot / 2 of the head, or 2 i and 2 i + 1
+ * (interleaved != 0); elements from rot on are copied.  Stretched positions
+ * (long contexts) are a matter of inv_freq and magnitude.
+ *
+ *   q, k, v    [tokens, hq or hk, d], dtype CP_BF16 or CP_F16; a token's heads
+ *              are contiguous, tokens are *_stride elements apart, so that
+ *              the three can be views of one projection's output.  q may be NULL.
+ *              Rows that are not 16-byte aligned are read element by element.
+ *   positions  [tokens] int32: kept tokens have the positions they had before
+ *              the prune, so there may be gaps
+ *   slots      [tokens] int64: page * page_size + offset, where each token's key
+ *              and value go; a negative slot, or one past the last page, stores
+ *              nothing.  Two tokens with one slot are the caller's error.
+ *   inv_freq   [rot / 2] float; rot even, 0 <= rot <= d <= 4096 (may be NULL when rot is 0)
+ *   q_out      [tokens, hq, d] dtype, dense; may be q where that is dense
+ *   k_cache, v_cache  [pages, hk, page_size, d], cache_dtype == dtype or CP_E4M3
+ *   k_scale, v_scale  [hk] float with CP_E4M3 (NULL: 1): what is stored is value / scale
+ */
+cp_status coverprune_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                               int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
+                               const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
+                               int32_t interleaved, float magnitude, void* q_out, void* k_cache, void* v_cache,
+                               cp_dtype cache_dtype, int64_t pages, int64_t page_size, const float* k_scale,
+                               const float* v_scale, void* stream);
+
+/* Attention of one new token of each sequence over its paged keys and values:
+ *   o = sum_j softmax_j(scale q . k_j) v_j over the sequence's tokens j.
+ *
+ *   q           [batch, hq, d] dtype CP_BF16 or CP_F16; d = 64, 96, 128, 192 or 256;
+ *               hq a multiple of hk, each run of hq / hk query heads reads one
+ *               key-value head
+ *   k_cache, v_cache  [pages, hk, page_size, d], cache_dtype == dtype or CP_E4M3;
+ *               slots that hold no token of the sequence may hold anything;
+ *               pages * hk * page_size < 2^32
+ *   k_scale, v_scale  [hk] float with CP_E4M3 (NULL: 1): what the stored values are times of
+ *   table       [batch, width] int32: the pages of each sequence in order
+ *               (entries outside [0, pages) are clamped; those that a length
+ *               does not reach are not read)
+ *   lengths     [batch] int32 tokens of each sequence, the new one included; 0
+ *               gives o = 0 and lse = -inf.  Lengths over max_length count as
+ *               max_length, negative ones as 0.
+ *   max_length  the longest length, known to the host; 1 <= max_length <= width * page_size
+ *   window      > 0: only the last `window` tokens count; 0: all
+ *   scale       finite; 1 / sqrt(d) is the usual choice
+ *   out         [batch, hq, d] dtype
+ *   lse         [batch, hq] float (may be NULL): log sum_j exp(scale q . k_j)
+ *   workspace   coverprune_paged_attention_workspace bytes (0 for bad sizes and
+ *               where none is needed): partial results of sequences cut into runs
+ */
+size_t coverprune_paged_attention_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
+                                            int64_t window);
+cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                     const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages,
+                                     int64_t page_size, const float* k_scale, const float* v_scale,
+                                     const int32_t* table, int64_t width, const int32_t* lengths, int64_t max_length,
+                                     int64_t window, float scale, void* out, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Measurement: the latency floor of one greedy step on this device (Sec. 3.5).

@@ -25,7 +25,7 @@ import torch
 
 __all__ = ["fst_cost", "fst_capacity", "prune", "sgs_select", "sgs_select_batch", "sgs_literal_select", "knn",
            "sgs_local_select", "lite_select", "uncovered_cost", "step_floor", "library", "library_path", "CoverPruneError",
-           "DEFAULT_KAPPA"]
+           "DEFAULT_KAPPA", "rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention"]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libcoverprune.so"
@@ -34,7 +34,7 @@ _LIB_NAME = "libcoverprune.so"
 DEFAULT_KAPPA = 10.0
 ABI_VERSION = 2
 
-CP_F32, CP_BF16 = 0, 1
+CP_F32, CP_BF16, CP_F16, CP_E4M3 = 0, 1, 2, 3
 CP_SGS_DENSE = 0
 CP_SGS_INCREMENTAL = 1
 CP_SGS_COMPACT = 2
@@ -163,6 +163,19 @@ def library() -> ctypes.CDLL:
     lib.coverprune_step_floor_workspace.restype = sz
     lib.coverprune_step_floor.argtypes = [vp, i64, i64, ctypes.c_int32, ctypes.c_int32, vp, sz, vp]
     lib.coverprune_step_floor.restype = st
+    f32, i32, dt = ctypes.c_float, ctypes.c_int32, ctypes.c_int
+    lib.coverprune_rms_norm.argtypes = [vp, dt, i64, i64, vp, vp, f32, vp, dt, vp, vp, vp]
+    lib.coverprune_rms_norm.restype = st
+    lib.coverprune_w4_matvec.argtypes = [vp, dt, vp, vp, vp, vp, i64, i64, i64, i64, dt, vp, dt, vp]
+    lib.coverprune_w4_matvec.restype = st
+    lib.coverprune_kv_append.argtypes = [vp, i64, vp, i64, vp, i64, dt, i64, i64, i64, i64, vp, vp, vp, i64, i32, f32, vp,
+                                         vp, vp, dt, i64, i64, vp, vp, vp]
+    lib.coverprune_kv_append.restype = st
+    lib.coverprune_paged_attention_workspace.argtypes = [i64, i64, i64, i64, i64, i64]
+    lib.coverprune_paged_attention_workspace.restype = sz
+    lib.coverprune_paged_attention.argtypes = [vp, dt, i64, i64, i64, i64, vp, vp, dt, i64, i64, vp, vp, vp, i64, vp, i64,
+                                               i64, f32, vp, vp, vp, sz, vp]
+    lib.coverprune_paged_attention.restype = st
     lib.coverprune_uncovered_cost.argtypes = [_Weights]
     lib.coverprune_uncovered_cost.restype = ctypes.c_float
     if lib.coverprune_abi_version() != ABI_VERSION:
@@ -566,3 +579,7 @@ def lite_select(feats: torch.Tensor, pos: torch.Tensor, frame: torch.Tensor, cap
                                       workspace.numel(), _stream(stream)))
     r = LiteResult(sel, group, obj, tc)
     return r.check(stream) if (check or _debug()) else r
+
+
+# The serving layer's operators use the helpers above.
+from .serving import RmsNormResult, kv_append, paged_attention, rms_norm, w4_matvec  # noqa: E402

@@ -613,4 +613,219 @@ cp_status coverprune_lite_select(const void* feats, cp_dtype dtype, int64_t n, i
   return ok();
 }
 
+// ---------------------------------------------------------------------------
+// Serving operators.
+
+static bool serve_type(cp_dtype t, cp::ServeType* out) {
+  switch (t) {
+    case CP_BF16: *out = cp::ServeType::kBf16; return true;
+    case CP_F16: *out = cp::ServeType::kF16; return true;
+    case CP_F32: *out = cp::ServeType::kF32; return true;
+    case CP_E4M3: *out = cp::ServeType::kE4m3; return true;
+  }
+  return false;
+}
+
+static bool half_type(cp_dtype t) { return t == CP_BF16 || t == CP_F16; }
+
+cp_status coverprune_rms_norm(const void* x, cp_dtype dtype, int64_t rows, int64_t d, const void* residual,
+                              const void* weight, float eps, void* out, cp_dtype out_dtype, float* out_scale,
+                              void* residual_out, void* stream) {
+  if (rows < 0 || rows >= (int64_t(1) << 31)) return fail(CP_ERR_INVALID_ARG, "rows = %lld outside [0, 2^31)", (long long)rows);
+  if (d < 1 || d > kMaxD) return fail(CP_ERR_INVALID_ARG, "d = %lld outside [1, %lld]", (long long)d, (long long)kMaxD);
+  if (!half_type(dtype) && dtype != CP_F32) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16, f16 or f32", (int)dtype);
+  if (out_dtype != dtype && out_dtype != CP_E4M3)
+    return fail(CP_ERR_UNSUPPORTED, "out_dtype %d: the input's type or e4m3", (int)out_dtype);
+  if (!std::isfinite(eps) || eps < 0.f) return fail(CP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (rows == 0) return ok();
+  if (!x || !weight || !out) return fail(CP_ERR_INVALID_ARG, "x, weight and out must be non-NULL");
+  if (residual && !residual_out) return fail(CP_ERR_INVALID_ARG, "residual_out is NULL with a residual");
+  if (out_dtype == CP_E4M3 && !out_scale) return fail(CP_ERR_INVALID_ARG, "out_scale is NULL with an e4m3 output");
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(out) || !aligned16(residual_out))
+    return fail(CP_ERR_INVALID_ARG, "x, residual, weight, out and residual_out must be 16-byte aligned");
+
+  cp::RmsNormParams p;
+  p.x = x;
+  p.residual = residual;
+  p.weight = weight;
+  p.out = out;
+  p.out_scale = out_scale;
+  p.residual_out = residual_out;
+  p.rows = rows;
+  p.d = int(d);
+  p.eps = eps;
+  serve_type(dtype, &p.type);
+  p.quantize = out_dtype == CP_E4M3;
+  hipError_t e = cp::launch_rms_norm(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "rms norm");
+  return ok();
+}
+
+cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_scale, const uint8_t* weight,
+                               const void* scale, const uint8_t* zero, int64_t m, int64_t n, int64_t k, int64_t group,
+                               cp_dtype dtype, void* y, cp_dtype y_dtype, void* stream) {
+  if (m < 0 || m > (int64_t(1) << 20)) return fail(CP_ERR_INVALID_ARG, "m = %lld outside [0, 2^20]", (long long)m);
+  if (n < 1 || n >= (int64_t(1) << 31)) return fail(CP_ERR_INVALID_ARG, "n = %lld outside [1, 2^31)", (long long)n);
+  if (k < 1 || k >= (int64_t(1) << 31)) return fail(CP_ERR_INVALID_ARG, "k = %lld outside [1, 2^31)", (long long)k);
+  if (group < 32 || group % 32 != 0 || k % group != 0)
+    return fail(CP_ERR_UNSUPPORTED, "group = %lld must be a multiple of 32 that divides k = %lld", (long long)group, (long long)k);
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if (x_dtype != dtype && x_dtype != CP_E4M3) return fail(CP_ERR_UNSUPPORTED, "x_dtype %d: dtype or e4m3", (int)x_dtype);
+  if (y_dtype != dtype && y_dtype != CP_F32) return fail(CP_ERR_UNSUPPORTED, "y_dtype %d: dtype or f32", (int)y_dtype);
+  if ((x_dtype == CP_E4M3) != (x_scale != nullptr))
+    return fail(CP_ERR_INVALID_ARG, "x_scale goes with an e4m3 x, and only with it");
+  if (m == 0) return ok();
+  if (!x || !weight || !scale || !y) return fail(CP_ERR_INVALID_ARG, "x, weight, scale and y must be non-NULL");
+  if (!aligned16(x) || !aligned16(weight) || !aligned16(scale) || !aligned16(y))
+    return fail(CP_ERR_INVALID_ARG, "x, weight, scale and y must be 16-byte aligned");
+
+  cp::W4Params p;
+  p.x = x;
+  p.x_scale = x_scale;
+  p.weight = weight;
+  p.scale = scale;
+  p.zero = zero;
+  p.y = y;
+  p.m = m;
+  p.n = n;
+  p.k = int(k);
+  p.group = int(group);
+  serve_type(dtype, &p.type);
+  serve_type(y_dtype, &p.y_type);
+  hipError_t e = cp::launch_w4_matvec(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "w4 matvec");
+  return ok();
+}
+
+cp_status coverprune_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                               int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
+                               const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
+                               int32_t interleaved, float magnitude, void* q_out, void* k_cache, void* v_cache,
+                               cp_dtype cache_dtype, int64_t pages, int64_t page_size, const float* k_scale,
+                               const float* v_scale, void* stream) {
+  if (tokens < 0 || tokens >= (int64_t(1) << 31))
+    return fail(CP_ERR_INVALID_ARG, "tokens = %lld outside [0, 2^31)", (long long)tokens);
+  if (hq < 0 || hq > 65536 || (q && hq < 1)) return fail(CP_ERR_INVALID_ARG, "hq = %lld outside [1, 65536]", (long long)hq);
+  if (hk < 1 || hk > 65536) return fail(CP_ERR_INVALID_ARG, "hk = %lld outside [1, 65536]", (long long)hk);
+  if (d < 1 || d > 4096) return fail(CP_ERR_INVALID_ARG, "d = %lld outside [1, 4096]", (long long)d);
+  if (rot < 0 || rot > d || rot % 2 != 0) return fail(CP_ERR_INVALID_ARG, "rot = %lld must be even, in [0, d]", (long long)rot);
+  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
+  if (pages < 1 || pages > (int64_t(1) << 40)) return fail(CP_ERR_INVALID_ARG, "pages = %lld outside [1, 2^40]", (long long)pages);
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if (cache_dtype != dtype && cache_dtype != CP_E4M3)
+    return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: dtype or e4m3", (int)cache_dtype);
+  if (cache_dtype != CP_E4M3 && (k_scale || v_scale)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e4m3 cache");
+  if (!std::isfinite(magnitude)) return fail(CP_ERR_INVALID_ARG, "magnitude must be finite");
+  if ((q && q_stride < hq * d) || k_stride < hk * d || v_stride < hk * d)
+    return fail(CP_ERR_INVALID_ARG, "a token stride is smaller than a token's heads");
+  if (tokens == 0) return ok();
+  if (!k || !v || !positions || !slots || !k_cache || !v_cache || (rot && !inv_freq) || (q && !q_out))
+    return fail(CP_ERR_INVALID_ARG, "k, v, positions, slots, inv_freq, k_cache, v_cache and (with q) q_out must be non-NULL");
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_out))
+    return fail(CP_ERR_INVALID_ARG, "k_cache, v_cache and q_out must be 16-byte aligned");
+
+  cp::KvAppendParams p;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.positions = positions;
+  p.slots = slots;
+  p.inv_freq = inv_freq;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.q_out = q_out;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.tokens = tokens;
+  p.pages = pages;
+  p.hq = int(hq);
+  p.hk = int(hk);
+  p.d = int(d);
+  p.rot = int(rot);
+  p.page = int(page_size);
+  p.magnitude = magnitude;
+  p.interleaved = interleaved != 0;
+  p.cache8 = cache_dtype == CP_E4M3;
+  serve_type(dtype, &p.type);
+  hipError_t e = cp::launch_kv_append(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kv append");
+  return ok();
+}
+
+static cp_status check_attend(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window) {
+  if (batch < 0 || batch > 65535) return fail(CP_ERR_INVALID_ARG, "batch = %lld outside [0, 65535]", (long long)batch);
+  if (hk < 1 || hq < 1 || hq > 65535 || hq % hk != 0)
+    return fail(CP_ERR_INVALID_ARG, "hq = %lld must be a multiple of hk = %lld, at most 65535", (long long)hq, (long long)hk);
+  if (d != 64 && d != 96 && d != 128 && d != 192 && d != 256)
+    return fail(CP_ERR_UNSUPPORTED, "d = %lld: 64, 96, 128, 192 or 256", (long long)d);
+  if (max_length < 1 || max_length >= (int64_t(1) << 31) - 64)
+    return fail(CP_ERR_INVALID_ARG, "max_length = %lld outside [1, 2^31 - 64)", (long long)max_length);
+  if (window < 0) return fail(CP_ERR_INVALID_ARG, "window = %lld must be >= 0", (long long)window);
+  return CP_OK;
+}
+
+size_t coverprune_paged_attention_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
+                                            int64_t window) {
+  if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
+  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window);
+}
+
+cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                     const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages,
+                                     int64_t page_size, const float* k_scale, const float* v_scale,
+                                     const int32_t* table, int64_t width, const int32_t* lengths, int64_t max_length,
+                                     int64_t window, float scale, void* out, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  cp_status st = check_attend(batch, hq, hk, d, max_length, window);
+  if (st != CP_OK) return st;
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if (cache_dtype != dtype && cache_dtype != CP_E4M3)
+    return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: dtype or e4m3", (int)cache_dtype);
+  if (cache_dtype != CP_E4M3 && (k_scale || v_scale)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e4m3 cache");
+  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
+  if (pages < 1 || pages > ((int64_t(1) << 32) - 1) / (hk * page_size))
+    return fail(CP_ERR_UNSUPPORTED, "pages = %lld: pages * hk * page_size must be in [1, 2^32)", (long long)pages);
+  if (width < 1 || width > (int64_t(1) << 31) / page_size || max_length > width * page_size)
+    return fail(CP_ERR_INVALID_ARG, "max_length = %lld over the table's %lld pages of %lld", (long long)max_length,
+                (long long)width, (long long)page_size);
+  if (!std::isfinite(scale)) return fail(CP_ERR_INVALID_ARG, "scale must be finite");
+  if (batch == 0) return ok();
+  if (!q || !k_cache || !v_cache || !table || !lengths || !out)
+    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, table, lengths and out must be non-NULL");
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
+    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache and out must be 16-byte aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window))) != CP_OK)
+    return st;
+
+  cp::AttendParams p;
+  p.q = q;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.table = table;
+  p.lengths = lengths;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.out = out;
+  p.lse = lse;
+  p.pages = pages;
+  p.max_length = max_length;
+  p.batch = int(batch);
+  p.hq = int(hq);
+  p.hk = int(hk);
+  p.d = int(d);
+  p.page = int(page_size);
+  p.width = int(width);
+  p.window = int(std::min<int64_t>(window, max_length));
+  p.scale = scale;
+  p.cache8 = cache_dtype == CP_E4M3;
+  serve_type(dtype, &p.type);
+  p.workspace = workspace;
+  hipError_t e = cp::launch_attend(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "paged attention");
+  return ok();
+}
+
 }  // extern "C"

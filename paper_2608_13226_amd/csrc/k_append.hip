@@ -1,0 +1,147 @@
+// Position rotation of queries and keys, and keys and values into a paged
+// cache, in one pass.
+//
+// Pair i of a head (elements i and i + R/2, or 2i and 2i + 1) turns by
+// position * inv_freq_i and grows by `magnitude`; elements from R on are
+// copied.  Bound by memory: every element is read and written once.  A block
+// works on one token: its R/2 angles go to LDS once and serve all heads.
+//
+// The angle is reduced to a fraction of a turn in float64 (32 bits of
+// position and 24 of frequency do not fit a float32 product, whose error
+// would reach whole hundredths of a radian at positions of 10^5), the sine
+// and cosine of the fraction are float32.
+#include "launch.h"
+#include "serve.h"
+
+namespace cp {
+namespace {
+
+// VEC consecutive elements of a head from element e on, into a query row or a
+// cache row.  `den` is the head's scale (e4m3 caches).
+template <class T, int VEC>
+__device__ __forceinline__ void load_run(const void* p, int64_t i, float* x) {
+  if constexpr (VEC == 8) load8<T>(p, i, x);
+  else x[0] = load1<T>(p, i);
+}
+template <class C, int VEC>
+__device__ __forceinline__ void store_run(void* p, int64_t i, float* x, float den) {
+  if constexpr (sizeof(C) == 1) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] /= den;
+  }
+  if constexpr (VEC == 8) store8<C>(p, i, x);
+  else store1<C>(p, i, x[0]);
+}
+
+// T: type of the projections, C: of the caches.  VEC = 8 needs 16-byte aligned
+// rows, d % 8 == 0 and pairs that come in whole runs (rot % 16 == 0, or 8
+// when interleaved); VEC = 1 is for everything else.
+template <class T, class C, int VEC, bool INTER>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p) {
+  extern __shared__ float s_turn[];           // [rot / 2] cosines, [rot / 2] sines
+  const int64_t t = blockIdx.x;
+  const int half = p.rot / 2;
+  const double position = double(p.positions[t]);
+  for (int i = threadIdx.x; i < half; i += blockDim.x) {
+    double turns = position * (double(p.inv_freq[i]) * 0.15915494309189533576888);
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.f * float(turns), &s, &c);
+    s_turn[i] = p.magnitude * c;
+    s_turn[half + i] = p.magnitude * s;
+  }
+  __syncthreads();
+
+  const int64_t slot = p.slots[t];
+  const bool keep = slot >= 0 && slot < p.pages * p.page;
+  const int64_t pg = keep ? slot / p.page : 0;
+  const int64_t off = keep ? slot - pg * p.page : 0;
+
+  // A head's work: runs of pairs (two runs of VEC elements, or VEC = 1
+  // interleaved pairs as two single ones), then runs of copied elements.
+  const bool split = !INTER || VEC == 1;
+  const int pair_runs = split ? half / VEC : p.rot / VEC;
+  const int runs = pair_runs + (p.d - p.rot) / VEC;
+  const int hq = p.q ? p.hq : 0;
+  const int total = (hq + p.hk) * runs;
+  for (int w = threadIdx.x; w < total; w += blockDim.x) {
+    const int head = w / runs, r = w - head * runs;
+    const bool is_q = head < hq;
+    const int kh = head - hq;
+    if (!is_q && !keep) continue;
+    const void* src = is_q ? p.q : p.k;
+    const int64_t from = is_q ? t * p.q_stride + int64_t(head) * p.d : t * p.k_stride + int64_t(kh) * p.d;
+    const int64_t to = is_q ? (t * p.hq + head) * p.d : ((pg * p.hk + kh) * p.page + off) * p.d;
+    const float den = (!is_q && p.k_scale) ? p.k_scale[kh] : 1.f;
+    auto put = [&](int e, float* x) {
+      if (is_q) store_run<T, VEC>(p.q_out, to + e, x, 1.f);
+      else store_run<C, VEC>(p.k_cache, to + e, x, den);
+    };
+    if (r >= pair_runs) {
+      const int e = p.rot + (r - pair_runs) * VEC;
+      float x[VEC];
+      load_run<T, VEC>(src, from + e, x);
+      put(e, x);
+    } else if (split) {
+      const int e1 = INTER ? 2 * r : r * VEC, e2 = INTER ? 2 * r + 1 : half + r * VEC;
+      float a[VEC], b[VEC];
+      load_run<T, VEC>(src, from + e1, a);
+      load_run<T, VEC>(src, from + e2, b);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float c = s_turn[r * VEC + j], s = s_turn[half + r * VEC + j];
+        const float x = a[j] * c - b[j] * s, y = b[j] * c + a[j] * s;
+        a[j] = x;
+        b[j] = y;
+      }
+      put(e1, a);
+      put(e2, b);
+    } else {
+      const int e = r * VEC;
+      float x[VEC];
+      load_run<T, VEC>(src, from + e, x);
+#pragma unroll
+      for (int j = 0; j + 1 < VEC; j += 2) {
+        const float c = s_turn[(e + j) / 2], s = s_turn[half + (e + j) / 2];
+        const float a = x[j] * c - x[j + 1] * s, b = x[j + 1] * c + x[j] * s;
+        x[j] = a;
+        x[j + 1] = b;
+      }
+      put(e, x);
+    }
+  }
+  if (!keep) return;
+  const int vruns = p.d / VEC;
+  for (int w = threadIdx.x; w < p.hk * vruns; w += blockDim.x) {
+    const int kh = w / vruns, e = (w - kh * vruns) * VEC;
+    float x[VEC];
+    load_run<T, VEC>(p.v, t * p.v_stride + int64_t(kh) * p.d + e, x);
+    store_run<C, VEC>(p.v_cache, ((pg * p.hk + kh) * p.page + off) * p.d + e, x, p.v_scale ? p.v_scale[kh] : 1.f);
+  }
+}
+
+template <class T, class C, int VEC, bool INTER>
+hipError_t launch(const KvAppendParams& p, hipStream_t stream) {
+  kv_append_kernel<T, C, VEC, INTER><<<dim3(unsigned(p.tokens)), dim3(256), size_t(p.rot) * sizeof(float), stream>>>(p);
+  return hipGetLastError();
+}
+
+bool aligned(const void* q, int64_t stride) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0 && stride % 8 == 0; }
+
+template <class T, class C>
+hipError_t launch_type(const KvAppendParams& p, hipStream_t stream) {
+  const bool wide = p.d % 8 == 0 && p.rot % (p.interleaved ? 8 : 16) == 0 && (!p.q || aligned(p.q, p.q_stride)) &&
+                    aligned(p.k, p.k_stride) && aligned(p.v, p.v_stride);
+  if (p.interleaved) return wide ? launch<T, C, 8, true>(p, stream) : launch<T, C, 1, true>(p, stream);
+  return wide ? launch<T, C, 8, false>(p, stream) : launch<T, C, 1, false>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendParams& p, hipStream_t stream) {
+  if (p.type == ServeType::kBf16)
+    return p.cache8 ? launch_type<Bf16, E4m3>(p, stream) : launch_type<Bf16, Bf16>(p, stream);
+  return p.cache8 ? launch_type<F16, E4m3>(p, stream) : launch_type<F16, F16>(p, stream);
+}
+
+}  // namespace cp

@@ -195,4 +195,82 @@ struct LiteParams {
 size_t lite_workspace_bytes(int64_t n, int64_t k);
 hipError_t launch_lite(const LiteParams& p, hipStream_t stream);
 
+// The serving operators.
+enum class ServeType { kBf16, kF16, kF32, kE4m3 };
+
+struct RmsNormParams {
+  const void* x;                  // [rows, d]
+  const void* residual;           // [rows, d] or nullptr
+  const void* weight;             // [d]
+  void* out;                      // [rows, d]
+  float* out_scale;               // [rows], with quantize
+  void* residual_out;             // [rows, d] with residual
+  int64_t rows;                   // 1 <= rows < 2^31
+  int d;                          // 1 <= d <= 65536
+  float eps;
+  ServeType type;                 // of x, residual, weight, residual_out; and of out unless quantize
+  bool quantize;                  // out is e4m3
+};
+hipError_t launch_rms_norm(const RmsNormParams& p, hipStream_t stream);
+
+// y = x (codes - zero) scale over groups of `group` consecutive k.
+struct W4Params {
+  const void* x;                  // [m, k], `type` or e4m3 (x_scale then set)
+  const float* x_scale;           // [m] or nullptr
+  const uint8_t* weight;          // [n, k / 2], two codes a byte, the even k low
+  const void* scale;              // [n, k / group] `type`
+  const uint8_t* zero;            // [n, k / group] or nullptr (8)
+  void* y;                        // [m, n]
+  int64_t m, n;
+  int k, group;                   // k % group == 0, group % 32 == 0
+  ServeType type;                 // kBf16 or kF16
+  ServeType y_type;               // `type` or kF32
+};
+hipError_t launch_w4_matvec(const W4Params& p, hipStream_t stream);
+
+struct KvAppendParams {
+  const void* q;                  // [tokens, hq, d] at token stride q_stride, or nullptr
+  const void* k;                  // [tokens, hk, d] at k_stride
+  const void* v;                  // [tokens, hk, d] at v_stride
+  int64_t q_stride, k_stride, v_stride;   // elements
+  const int32_t* positions;       // [tokens]
+  const int64_t* slots;           // [tokens]
+  const float* inv_freq;          // [rot / 2]
+  const float* k_scale;           // [hk] or nullptr, e4m3 caches
+  const float* v_scale;
+  void* q_out;                    // [tokens, hq, d], with q
+  void* k_cache;                  // [pages, hk, page, d]
+  void* v_cache;
+  int64_t tokens, pages;
+  int hq, hk, d, rot, page;
+  float magnitude;
+  bool interleaved;
+  bool cache8;                    // caches are e4m3
+  ServeType type;
+};
+hipError_t launch_kv_append(const KvAppendParams& p, hipStream_t stream);
+
+struct AttendParams {
+  const void* q;                  // [batch, hq, d]
+  const void* k_cache;            // [pages, hk, page, d]
+  const void* v_cache;
+  const int32_t* table;           // [batch, width]
+  const int32_t* lengths;         // [batch]
+  const float* k_scale;           // [hk] or nullptr, e4m3 caches
+  const float* v_scale;
+  void* out;                      // [batch, hq, d]
+  float* lse;                     // [batch, hq] or nullptr
+  int64_t pages;                  // pages * hk * page < 2^32
+  int64_t max_length;             // 1 <= max_length <= width * page < 2^31
+  int batch, hq, hk, d, page, width;
+  int window;                     // 0: none
+  float scale;
+  bool cache8;
+  ServeType type;
+  void* workspace;
+};
+// 0 where one launch writes the result.
+size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window);
+hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
+
 }  // namespace cp

@@ -1,0 +1,100 @@
+"""coverprune_rms_norm against its float64 statement."""
+import pytest
+
+from tests import serving_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def _data(rows, d, t, residual, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed + 7 * rows + d)
+    x = torch.randn(rows, d, device="cuda", generator=g).to(t)
+    w = (1.0 + 0.3 * torch.randn(d, device="cuda", generator=g)).to(t)
+    r = (3.0 * torch.randn(rows, d, device="cuda", generator=g)).to(t) if residual else None
+    return x, w, r
+
+
+def _check(x, w, r, eps, got, quantize):
+    d = x.shape[1]
+    y, h = ref.rms_norm(x, w, eps, r)
+    # The sum of squares in float32: lanes add up to 64 values each, then a tree.
+    work = 2.0 ** -24 * (64 + 16) * y.abs()
+    if r is not None:
+        ref.assert_close(got.residual, h, x.dtype, 2.0 ** -24 * h.abs(), f"residual d={d}")
+    else:
+        assert got.residual is None
+    if not quantize:
+        assert got.scale is None
+        ref.assert_close(got.out, y, x.dtype, work, f"norm d={d}")
+        return
+    scale = y.abs().amax(1) / 448.0
+    ref.assert_close(got.scale, scale, F32, 2.0 ** -24 * 96 * scale, f"scale d={d}")
+    s = got.scale.cpu().double()[:, None]
+    ref.assert_e4m3(got.out, torch.where(s == 0, torch.zeros_like(y), y / s), f"codes d={d}")
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("t", [BF, F16, F32])
+@pytest.mark.parametrize("rows,d", [(1, 1), (3, 7), (1, 8), (5, 96), (300, 1000), (1, 3584), (33, 3584), (2, 4097),
+                                    (2, 8192), (3, 20001), (2, 65536), (700, 129), (1030, 64), (2050, 512)])
+def test_norm(rows, d, t, residual, quantize):
+    import paper_2608_13226_amd as cp
+    print(f"norm rows={rows} d={d} {t} residual={residual} quantize={quantize}", flush=True)
+    x, w, r = _data(rows, d, t, residual)
+    got = cp.rms_norm(x, w, eps=1e-5, residual=r, quantize=quantize)
+    _check(x, w, r, 1e-5, got, quantize)
+
+
+def test_rows_of_nothing_and_zeros():
+    import paper_2608_13226_amd as cp
+    x, w, r = _data(0, 3584, BF, True)
+    got = cp.rms_norm(x, w, residual=r, quantize=True)
+    assert got.out.shape == (0, 3584) and got.scale.shape == (0,)
+    x, w, _ = _data(3, 520, BF, False)
+    x[1] = 0
+    got = cp.rms_norm(x, w, eps=1e-6, quantize=True)
+    _check(x, w, None, 1e-6, got, True)
+    assert float(got.scale[1]) == 0.0 and not d64_any(got.out[1])
+
+
+def d64_any(t):
+    return bool((ref.d64(t) != 0).any())
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_bad_row_stays_alone(bad):
+    """An infinite or NaN element spoils its own row (as in the formula) and no other."""
+    import paper_2608_13226_amd as cp
+    x, w, _ = _data(9, 1000, BF, False)
+    clean = cp.rms_norm(x, w, quantize=True)
+    x[4, 333] = bad
+    got = cp.rms_norm(x, w, quantize=True)
+    keep = [i for i in range(9) if i != 4]
+    assert torch.equal(got.scale[keep], clean.scale[keep])
+    assert torch.equal(got.out.view(torch.uint8)[keep], clean.out.view(torch.uint8)[keep])
+    assert bool(torch.isnan(got.scale[4]))
+    y = cp.rms_norm(x, w).out.float()
+    assert bool(torch.isnan(y[4, 333])) and bool(torch.isfinite(y[keep]).all())
+
+
+def test_update_in_place_and_given_outputs():
+    import paper_2608_13226_amd as cp
+    x, w, r = _data(65, 3584, BF, True)
+    want = cp.rms_norm(x, w, residual=r)
+    mine = r.clone()
+    out = torch.empty_like(x)
+    got = cp.rms_norm(x, w, residual=mine, residual_out=mine, out=out)
+    assert got.out.data_ptr() == out.data_ptr() and torch.equal(out, want.out) and torch.equal(mine, want.residual)
+
+
+def test_large_values_do_not_overflow_the_output_scale():
+    import paper_2608_13226_amd as cp
+    x, w, _ = _data(4, 2048, F32, False)
+    x = x * 1e15
+    x[2] *= 1e-30
+    got = cp.rms_norm(x, w, eps=0.0, quantize=True)
+    _check(x, w, None, 0.0, got, True)

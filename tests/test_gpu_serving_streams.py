@@ -1,0 +1,77 @@
+"""The serving operators on a stream of their own and in a replayed graph: one
+decode step, norm -> product -> append -> attention -> product."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF = torch.bfloat16
+
+
+class _Step:
+    def __init__(self, batch=3, length=900, seed=0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.hq, self.hk, self.d, self.page = 8, 2, 128, 16
+        dim, width = self.hq * self.d, (length + 15) // 16 + 1
+
+        def w4(n, k):
+            return (torch.randint(0, 256, (n, k // 2), device="cuda", generator=g, dtype=torch.uint8),
+                    (0.01 + 0.01 * torch.rand(n, k // 128, device="cuda", generator=g)).to(BF))
+
+        self.x = torch.randn(batch, dim, device="cuda", generator=g).to(BF)
+        self.h = torch.randn(batch, dim, device="cuda", generator=g).to(BF)
+        self.gain = torch.ones(dim, device="cuda", dtype=BF)
+        self.wqkv, self.wo = w4((self.hq + 2 * self.hk) * self.d, dim), w4(dim, dim)
+        self.k, self.v = (torch.randn(batch * width, self.hk, 16, self.d, device="cuda", generator=g).to(BF) for _ in range(2))
+        self.table = torch.arange(batch * width, device="cuda", dtype=torch.int32).view(batch, width)
+        self.lengths = torch.full((batch,), length, device="cuda", dtype=torch.int32)
+        self.positions = self.lengths * 7
+        at = self.lengths.long() - 1
+        self.slots = self.table.long().gather(1, (at // 16)[:, None])[:, 0] * 16 + at % 16
+        self.inv = 10000.0 ** (-torch.arange(0, self.d, 2, device="cuda") / self.d)
+        self.length = length
+
+    def __call__(self):
+        import paper_2608_13226_amd as cp
+        r = cp.rms_norm(self.x, self.gain, residual=self.h, quantize=True)
+        qkv = cp.w4_matvec(r.out, *self.wqkv, x_scale=r.scale).unflatten(1, (-1, self.d))
+        q, k, v = qkv.split([self.hq, self.hk, self.hk], 1)
+        q = cp.kv_append(q, k, v, self.positions, self.slots, self.inv, self.k, self.v)
+        o = cp.paged_attention(q, self.k, self.v, self.table, self.lengths, max_length=self.length)
+        return cp.w4_matvec(o.flatten(1), *self.wo), r.residual
+
+
+def test_on_another_stream():
+    step = _Step()
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = step()
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("length", [900, 20000])
+def test_in_a_graph(length):
+    step = _Step(length=length)
+    step()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(4):
+        # New inputs in place, eager work and a synchronization between the replays.
+        g = torch.Generator(device="cuda").manual_seed(100 + i)
+        step.x.copy_(torch.randn(step.x.shape, device="cuda", generator=g))
+        step.positions.add_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {i}"

@@ -1,0 +1,98 @@
+"""coverprune_w4_matvec against its float64 statement."""
+import pytest
+
+from tests import serving_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF, F16, F32, E4M3 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn
+
+
+def _data(m, n, k, group, t, x8, zero, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed + m + 31 * n + 7 * k)
+    x = torch.randn(m, k, device="cuda", generator=g)
+    xs = None
+    if x8:
+        xs = 0.01 + torch.rand(m, device="cuda", generator=g)
+        x = (60.0 * x).clamp(-448, 448).to(E4M3)
+    else:
+        x = x.to(t)
+    w = torch.randint(0, 256, (n, k // 2), device="cuda", generator=g, dtype=torch.uint8)
+    s = (0.05 * torch.randn(n, k // group, device="cuda", generator=g)).to(t)
+    z = torch.randint(0, 16, (n, k // group), device="cuda", generator=g, dtype=torch.uint8) if zero else None
+    return x, w, s, z, xs
+
+
+def _check(x, w, s, z, xs, out_dtype=None):
+    import paper_2608_13226_amd as cp
+    y = cp.w4_matvec(x, w, s, zero=z, x_scale=xs, out_dtype=out_dtype)
+    want, work = ref.w4_matvec(x, w, s, z, xs)
+    assert y.shape == want.shape and y.dtype == (out_dtype or s.dtype)
+    ref.assert_close(y, want, y.dtype, work, f"m={x.shape[0]} n={w.shape[0]} k={x.shape[1]}")
+    return y
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("t", [BF, F16])
+@pytest.mark.parametrize("m,n,k,group", [
+    (1, 1, 32, 32), (1, 16, 64, 32), (2, 33, 96, 96), (3, 15, 160, 32), (1, 128, 128, 128), (7, 48, 384, 128),
+    (15, 17, 256, 256), (16, 100, 192, 64), (17, 64, 512, 128), (5, 1500, 1184, 32), (33, 130, 640, 64),
+    (64, 257, 1024, 128), (65, 96, 320, 160), (130, 40, 896, 128), (1, 4608, 3584, 128), (4, 70, 4480, 4480),
+    (9, 96, 2112, 96), (24, 300, 7168, 256)])
+def test_products(m, n, k, group, t, x8):
+    zero = (m + n) % 2 == 1
+    print(f"w4 m={m} n={n} k={k} group={group} {t} x8={x8} zero={zero}", flush=True)
+    data = _data(m, n, k, group, t, x8, zero)
+    _check(*data)
+    _check(*data, out_dtype=F32)
+
+
+def test_every_code_and_place():
+    """One row of x picks single codes out: every code value at every place of a 128-run."""
+    import paper_2608_13226_amd as cp
+    for t in (BF, F16):
+        for group in (32, 128):
+            k = n = 256
+            codes = (torch.arange(n, device="cuda")[:, None] * 7 + torch.arange(k, device="cuda")) % 16
+            w = (codes[:, 0::2] | codes[:, 1::2] << 4).to(torch.uint8)
+            s = torch.ones(n, k // group, device="cuda", dtype=t)
+            y = cp.w4_matvec(torch.eye(k, device="cuda", dtype=t), w, s, out_dtype=F32)
+            assert torch.equal(y, (codes - 8).t().float()), (t, group)
+
+
+def test_no_rows():
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(0, 32, 128, 128, BF, False, True)
+    assert cp.w4_matvec(x, w, s, zero=z).shape == (0, 32)
+
+
+def test_rows_do_not_touch_each_other():
+    """NaN or infinity in one row of x reaches that row's results only."""
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(20, 100, 512, 128, BF, False, True)
+    clean = cp.w4_matvec(x, w, s, zero=z)
+    x[3, 7], x[18, 500] = float("nan"), float("inf")
+    y = cp.w4_matvec(x, w, s, zero=z)
+    keep = [i for i in range(20) if i not in (3, 18)]
+    assert torch.equal(y[keep], clean[keep])
+    assert not bool(torch.isfinite(y[3].float()).any())
+
+
+def test_the_same_answer_every_time():
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(64, 1000, 3584, 128, BF, False, True)
+    y = cp.w4_matvec(x, w, s, zero=z)
+    for _ in range(5):
+        assert torch.equal(cp.w4_matvec(x, w, s, zero=z), y)
+
+
+def test_fed_by_the_norm():
+    """The norm's 8-bit rows and scales are what the product takes."""
+    import paper_2608_13226_amd as cp
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(6, 1024, device="cuda", generator=g).to(BF)
+    gain = torch.ones(1024, device="cuda", dtype=BF)
+    r = cp.rms_norm(x, gain, quantize=True)
+    _, w, s, z, _ = _data(6, 200, 1024, 128, BF, False, True)
+    _check(r.out, w, s, z, r.scale, out_dtype=F32)
