@@ -260,25 +260,63 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int
   }
 }
 
-// The runs of one (sequence, query head) joined.
-template <class T>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p, int runs, const float* part_o, const float* part_ml) {
+// The runs of one (sequence, query head) joined.  The runs' weights are found
+// once, in LDS; then D / 4 threads read a run's row and the block's other
+// threads read other runs', so a long sequence's rows are in flight together.
+constexpr int kJoinThreads = 512;
+template <class T, int D>
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams p, int runs, const float* part_o,
+                                                                   const float* part_ml) {
+  constexpr int kLanes = D / 4, kRows = kJoinThreads / kLanes;
+  extern __shared__ float s_f[];                // [runs] weights
+  __shared__ float s_red[kJoinThreads / kWave];
+  __shared__ f32x4 s_acc[kRows][kLanes];
   const int64_t row = blockIdx.x;
-  const int d = threadIdx.x;
-  const float* ml = part_ml + row * runs * 2;
+  const int tid = threadIdx.x;
+  const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * runs;
   float M = -INFINITY;
-  for (int s = 0; s < runs; ++s)
-    if (ml[2 * s + 1] != 0.f) M = fmaxf(M, ml[2 * s]);
-  float acc = 0.f, sum = 0.f;
-  for (int s = 0; s < runs; ++s) {
-    if (ml[2 * s + 1] == 0.f) continue;
-    const float f = exp2f(ml[2 * s] - M);
-    sum = fmaf(ml[2 * s + 1], f, sum);
-    acc = fmaf(part_o[(row * runs + s) * p.d + d], f, acc);
+  for (int s = tid; s < runs; s += kJoinThreads) {
+    const float2 v = ml[s];
+    if (v.y != 0.f) M = fmaxf(M, v.x);
   }
-  const float vs = p.v_scale ? p.v_scale[row % p.hq / (p.hq / p.hk)] : 1.f;
-  store1<T>(p.out, row * p.d + d, sum == 0.f ? 0.f : acc / sum * vs);
-  if (p.lse && d == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  M = wave_max(M);
+  if (tid % kWave == 0) s_red[tid / kWave] = M;
+  __syncthreads();
+  M = s_red[0];
+#pragma unroll
+  for (int w = 1; w < kJoinThreads / kWave; ++w) M = fmaxf(M, s_red[w]);
+  __syncthreads();
+  float sum = 0.f;
+  for (int s = tid; s < runs; s += kJoinThreads) {
+    const float2 v = ml[s];
+    const float f = v.y != 0.f ? exp2f(v.x - M) : 0.f;
+    s_f[s] = f;
+    sum = v.y != 0.f ? fmaf(v.y, f, sum) : sum;
+  }
+  sum = wave_sum(sum);
+  if (tid % kWave == 0) s_red[tid / kWave] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / kWave; ++w) sum += s_red[w];
+
+  const int r = tid / kLanes, c = tid % kLanes;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (r < kRows) {
+    const f32x4* o = reinterpret_cast<const f32x4*>(part_o + row * runs * D) + c;
+    for (int s = r; s < runs; s += kRows) acc += o[int64_t(s) * kLanes] * s_f[s];
+    s_acc[r][c] = acc;
+  }
+  __syncthreads();
+  if (r != 0) return;
+#pragma unroll
+  for (int i = 1; i < kRows; ++i) acc += s_acc[i][c];
+  const float k = sum == 0.f ? 0.f : (p.v_scale ? p.v_scale[row % p.hq / (p.hq / p.hk)] : 1.f) / sum;
+  u32x2 w;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) w[i] = sum == 0.f ? 0u : pack2<T>(acc[2 * i] * k, acc[2 * i + 1] * k);
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + c * 4) = w;
+  if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
 // How the tokens of the longest sequence are cut: about four blocks a compute
@@ -311,7 +349,7 @@ hipError_t launch(const AttendParams& p, hipStream_t stream) {
   attend_kernel<T, C8, D><<<grid, dim3(64 * kWaves), 0, stream>>>(p, c.tiles_per_run, c.runs, part_o, part_ml);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || c.runs == 1) return e;
-  attend_join_kernel<T><<<dim3(unsigned(rows)), dim3(D), 0, stream>>>(p, c.runs, part_o, part_ml);
+  attend_join_kernel<T, D><<<dim3(unsigned(rows)), dim3(kJoinThreads), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml);
   return hipGetLastError();
 }
 

@@ -2,41 +2,49 @@
 tokens: norm, 4-bit products, append to a paged cache, attention over it.
 
 As in the rest of the binding, the functions only check and marshal torch
-tensors.  Each takes tensors of the current GPU, enqueues on torch's current
-stream (or ``stream``) and returns without waiting; outputs that are not given
-are allocated.  8-bit tensors are torch.float8_e4m3fn throughout.
+tensors; here that part is compiled (csrc/binding.cpp), because a decode step
+is a handful of calls of a few microseconds each.  Each takes tensors of the
+current GPU, enqueues on torch's current stream (or ``stream``) and returns
+without waiting; outputs that are not given are allocated.  8-bit tensors are
+torch.float8_e4m3fn throughout.  Wrong types raise TypeError, wrong shapes,
+strides and devices ValueError, what the library itself refuses
+CoverPruneError.
 """
 from __future__ import annotations
 
-import math
+import os
 from typing import NamedTuple, Optional
 
 import torch
 
-from . import CP_BF16, CP_E4M3, CP_F16, CP_F32, _check, _need, _workspace, library
+from . import HERE, CoverPruneError, library
 
 __all__ = ["rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention"]
 
-E4M3 = torch.float8_e4m3fn
-_CODE = {torch.float32: CP_F32, torch.bfloat16: CP_BF16, torch.float16: CP_F16, E4M3: CP_E4M3}
-_HALF = (torch.bfloat16, torch.float16)
+
+class _Unloaded:
+    """Stands for the compiled half until the first call, which loads it."""
+
+    def __getattr__(self, name):
+        global _native
+        library()
+        if not os.path.exists(os.path.join(HERE, "_serving.so")):
+            raise CoverPruneError(f"{os.path.join(HERE, '_serving.so')} is missing: build it with "
+                                  f"`python -m paper_2608_13226_amd.build`")
+        from . import _serving
+        _serving.init(CoverPruneError, _raw_stream)
+        _native = _serving
+        return getattr(_serving, name)
 
 
-def _at(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
+def _any_raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
 
 
-def _on(stream, dev) -> int:
-    if dev.type != "cuda":
-        raise ValueError(f"tensors must be on the GPU, got {dev}")
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-
-
-def _scales(t, name, n, dev, eight):
-    if t is not None:
-        if not eight:
-            raise ValueError(f"{name} goes with 8-bit values")
-        _need(t, name, torch.float32, (n,), dev)
+# torch's own function for the handle of a device's current stream, where it
+# has one: a fifth of the time of making a Stream object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _any_raw_stream)
+_native = _Unloaded()
 
 
 class RmsNormResult(NamedTuple):
@@ -50,39 +58,14 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
              residual_out: Optional[torch.Tensor] = None, stream=None) -> RmsNormResult:
     """Root-mean-square norm of the rows of x (+ residual), times weight.
 
+    x, residual [rows, d] and weight [d] are bfloat16, float16 or float32.
     quantize=True rounds to float8_e4m3fn with a scale per row (max / 448), the
     input that w4_matvec takes with x_scale.  residual_out may be residual
     itself (an update in place)."""
-    if x.dim() != 2:
-        raise ValueError("x must be [rows, d]")
-    rows, d = x.shape
-    dev, t = x.device, x.dtype
-    if t not in _HALF and t != torch.float32:
-        raise TypeError(f"x must be bfloat16, float16 or float32, got {t}")
-    _need(x, "x", t, (rows, d), dev)
-    _need(weight, "weight", t, (d,), dev)
-    ot = E4M3 if quantize else t
-    if out is None:
-        out = torch.empty((rows, d), dtype=ot, device=dev)
-    else:
-        _need(out, "out", ot, (rows, d), dev)
-    if residual is None:
-        residual_out = None
-    else:
-        _need(residual, "residual", t, (rows, d), dev)
-        if residual_out is None:
-            residual_out = torch.empty((rows, d), dtype=t, device=dev)
-        else:
-            _need(residual_out, "residual_out", t, (rows, d), dev)
-    if not quantize:
-        out_scale = None
-    elif out_scale is None:
-        out_scale = torch.empty(rows, dtype=torch.float32, device=dev)
-    else:
-        _need(out_scale, "out_scale", torch.float32, (rows,), dev)
-    _check(library().coverprune_rms_norm(_at(x), _CODE[t], rows, d, _at(residual), _at(weight), eps, _at(out), _CODE[ot],
-                                         _at(out_scale), _at(residual_out), _on(stream, dev)))
-    return RmsNormResult(out, out_scale, residual_out)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm(x, weight, eps, residual, quantize, out, out_scale, residual_out)
+    return RmsNormResult._make(_native.rms_norm(x, weight, eps, residual, quantize, out, out_scale, residual_out))
 
 
 def w4_matvec(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor] = None,
@@ -91,72 +74,14 @@ def w4_matvec(x: torch.Tensor, weight: torch.Tensor, scale: torch.Tensor, zero: 
     """x [m, k] times 4-bit weights [n, k]: y[i, o] = sum_j x[i, j] (code[o, j] - zero) scale.
 
     weight: [n, k / 2] uint8, two codes a byte, the even j in the low half;
-    scale: [n, k / group] bfloat16 or float16; zero: [n, k / group] uint8 codes
-    (8 without).  x has scale's type, or is float8_e4m3fn with x_scale [m].
-    out_dtype: scale's type (default) or float32."""
-    if x.dim() != 2 or weight.dim() != 2 or scale.dim() != 2:
-        raise ValueError("x, weight and scale must be matrices")
-    m, k = x.shape
-    n, groups = scale.shape
-    dev, t = x.device, scale.dtype
-    if t not in _HALF:
-        raise TypeError(f"scale must be bfloat16 or float16, got {t}")
-    if x.dtype != t and x.dtype != E4M3:
-        raise TypeError(f"x must be {t} or {E4M3}, got {x.dtype}")
-    if groups < 1 or k % groups != 0:
-        raise ValueError(f"scale has {groups} groups for k = {k}")
-    _need(x, "x", x.dtype, (m, k), dev)
-    _need(weight, "weight", torch.uint8, (n, k // 2), dev)
-    _need(scale, "scale", t, (n, groups), dev)
-    if zero is not None:
-        _need(zero, "zero", torch.uint8, (n, groups), dev)
-    if (x_scale is not None) != (x.dtype == E4M3):
-        raise ValueError("x_scale goes with an 8-bit x, and only with it")
-    if x_scale is not None:
-        _need(x_scale, "x_scale", torch.float32, (m,), dev)
-    yt = t if out_dtype is None else out_dtype
-    if yt != t and yt != torch.float32:
-        raise TypeError(f"out_dtype must be {t} or float32, got {yt}")
-    if out is None:
-        out = torch.empty((m, n), dtype=yt, device=dev)
-    else:
-        _need(out, "out", yt, (m, n), dev)
-    _check(library().coverprune_w4_matvec(_at(x), _CODE[x.dtype], _at(x_scale), _at(weight), _at(scale), _at(zero), m, n, k,
-                                          k // groups, _CODE[t], _at(out), _CODE[yt], _on(stream, dev)))
-    return out
-
-
-def _heads(x, name, t, tokens, d, dev):
-    """A [tokens, heads, d] view whose heads are contiguous; returns its head count and token stride."""
-    if x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != d:
-        raise ValueError(f"{name} must be [{tokens}, heads, {d}], got {tuple(x.shape)}")
-    if x.dtype != t:
-        raise TypeError(f"{name} must be {t}, got {x.dtype}")
-    if x.device != dev:
-        raise ValueError(f"{name} must be on {dev}, got {x.device}")
-    heads = x.shape[1]
-    stride, head_stride, one = x.stride()
-    if (one != 1 and d > 1) or (head_stride != d and heads > 1):
-        raise ValueError(f"{name}: a token's heads must be contiguous")
-    if tokens < 2:
-        stride = heads * d
-    elif stride < heads * d:
-        raise ValueError(f"{name}: tokens overlap")
-    return heads, stride
-
-
-def _caches(k_cache, v_cache, t, hk, d, dev, k_scale, v_scale):
-    if k_cache.dim() != 4:
-        raise ValueError("the caches must be [pages, heads, page_size, d]")
-    pages, _, page, _ = k_cache.shape
-    c = k_cache.dtype
-    if c != t and c != E4M3:
-        raise TypeError(f"the caches must be {t} or {E4M3}, got {c}")
-    _need(k_cache, "k_cache", c, (pages, hk, page, d), dev)
-    _need(v_cache, "v_cache", c, (pages, hk, page, d), dev)
-    _scales(k_scale, "k_scale", hk, dev, c == E4M3)
-    _scales(v_scale, "v_scale", hk, dev, c == E4M3)
-    return c, pages, page
+    scale: [n, k / group] bfloat16 or float16, groups of a multiple of 32;
+    zero: [n, k / group] uint8 codes (8 without).  x has scale's type, or is
+    float8_e4m3fn with x_scale [m] float32.  out_dtype: scale's type (default)
+    or float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return w4_matvec(x, weight, scale, zero, x_scale, out_dtype, out)
+    return _native.w4_matvec(x, weight, scale, zero, x_scale, out_dtype, out)
 
 
 def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
@@ -172,38 +97,10 @@ def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, posit
     (negative: not stored); inv_freq [rot / 2] float32, rot <= d elements of
     each head are rotated (None: none); caches [pages, heads, page_size, d] of
     k's type, or float8_e4m3fn holding value / k_scale[head], v_scale[head]."""
-    t = k.dtype
-    if t not in _HALF:
-        raise TypeError(f"k must be bfloat16 or float16, got {t}")
-    if k.dim() != 3:
-        raise ValueError("k must be [tokens, heads, d]")
-    tokens, hk, d = k.shape
-    dev = k.device
-    _, ks = _heads(k, "k", t, tokens, d, dev)
-    hv, vs = _heads(v, "v", t, tokens, d, dev)
-    if hv != hk:
-        raise ValueError(f"v has {hv} heads, k has {hk}")
-    hq, qs = 0, 0
-    if q is not None:
-        hq, qs = _heads(q, "q", t, tokens, d, dev)
-        if q_out is None:
-            q_out = torch.empty((tokens, hq, d), dtype=t, device=dev)
-        else:
-            _need(q_out, "q_out", t, (tokens, hq, d), dev)
-    else:
-        q_out = None
-    _need(positions, "positions", torch.int32, (tokens,), dev)
-    _need(slots, "slots", torch.int64, (tokens,), dev)
-    half = 0
-    if inv_freq is not None:
-        half = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
-        _need(inv_freq, "inv_freq", torch.float32, (half,), dev)
-    c, pages, page = _caches(k_cache, v_cache, t, hk, d, dev, k_scale, v_scale)
-    _check(library().coverprune_kv_append(_at(q), qs, _at(k), ks, _at(v), vs, _CODE[t], tokens, hq, hk, d, _at(positions),
-                                          _at(slots), _at(inv_freq), 2 * half, bool(interleaved), magnitude, _at(q_out),
-                                          _at(k_cache), _at(v_cache), _CODE[c], pages, page, _at(k_scale), _at(v_scale),
-                                          _on(stream, dev)))
-    return q_out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_append(q, k, v, positions, slots, inv_freq, k_cache, v_cache, interleaved, magnitude, k_scale, v_scale, q_out)
+    return _native.kv_append(q, k, v, positions, slots, inv_freq, k_cache, v_cache, interleaved, magnitude, k_scale, v_scale, q_out)
 
 
 def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -220,36 +117,9 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     the host (default: all that the table can hold, which cuts short sequences
     into more pieces than they need).  window > 0: only the last `window`
     tokens.  scale defaults to 1 / sqrt(d)."""
-    t = q.dtype
-    if t not in _HALF:
-        raise TypeError(f"q must be bfloat16 or float16, got {t}")
-    if q.dim() != 3 or table.dim() != 2 or k_cache.dim() != 4:
-        raise ValueError("q must be [batch, heads, d], table [batch, width], the caches [pages, heads, page_size, d]")
-    batch, hq, d = q.shape
-    dev, hk, width = q.device, k_cache.shape[1], table.shape[1]
-    _need(q, "q", t, (batch, hq, d), dev)
-    c, pages, page = _caches(k_cache, v_cache, t, hk, d, dev, k_scale, v_scale)
-    _need(table, "table", torch.int32, (batch, width), dev)
-    _need(lengths, "lengths", torch.int32, (batch,), dev)
-    if out is None:
-        out = torch.empty((batch, hq, d), dtype=t, device=dev)
-    else:
-        _need(out, "out", t, (batch, hq, d), dev)
-    if lse is not None:
-        _need(lse, "lse", torch.float32, (batch, hq), dev)
-    elif return_lse:
-        lse = torch.empty((batch, hq), dtype=torch.float32, device=dev)
-    if max_length is None:
-        max_length = width * page
-    if scale is None:
-        scale = 1.0 / math.sqrt(d)
-    lib = library()
-    if workspace is None:
-        need = lib.coverprune_paged_attention_workspace(batch, hq, hk, d, max_length, window)
-        if need:
-            workspace = _workspace(need, dev)
-    _check(lib.coverprune_paged_attention(_at(q), _CODE[t], batch, hq, hk, d, _at(k_cache), _at(v_cache), _CODE[c], pages, page,
-                                          _at(k_scale), _at(v_scale), _at(table), width, _at(lengths), max_length, window,
-                                          scale, _at(out), _at(lse), _at(workspace),
-                                          0 if workspace is None else workspace.numel(), _on(stream, dev)))
-    return (out, lse) if return_lse else out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return paged_attention(q, k_cache, v_cache, table, lengths, max_length, window, scale, k_scale, v_scale, return_lse,
+                                   out, lse, workspace)
+    return _native.paged_attention(q, k_cache, v_cache, table, lengths, max_length, window, scale, k_scale, v_scale, return_lse,
+                                   out, lse, workspace)
