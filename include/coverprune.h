@@ -532,7 +532,7 @@ cp_status coverprune_rms_norm(const void* x, cp_dtype dtype, int64_t rows, int64
  *   weight   [n, k / 2] bytes, two 4-bit codes each, the even j in the low half
  *   scale    [n, k / group] dtype
  *   zero     [n, k / group] bytes, the code that stands for 0; NULL: 8
- *   group    a multiple of 32 that divides k (k < 2^31)
+ *   group    a multiple of 32 that divides k (k <= 2^20)
  *   dtype    CP_BF16 or CP_F16
  *   y        [m, n], y_dtype == dtype or CP_F32
  * The time is that of reading the weights up to m = 16; every further 64 rows

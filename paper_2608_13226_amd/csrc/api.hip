@@ -666,7 +666,7 @@ cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_s
                                cp_dtype dtype, void* y, cp_dtype y_dtype, void* stream) {
   if (m < 0 || m > (int64_t(1) << 20)) return fail(CP_ERR_INVALID_ARG, "m = %lld outside [0, 2^20]", (long long)m);
   if (n < 1 || n >= (int64_t(1) << 31)) return fail(CP_ERR_INVALID_ARG, "n = %lld outside [1, 2^31)", (long long)n);
-  if (k < 1 || k >= (int64_t(1) << 31)) return fail(CP_ERR_INVALID_ARG, "k = %lld outside [1, 2^31)", (long long)k);
+  if (k < 1 || k > (int64_t(1) << 20)) return fail(CP_ERR_INVALID_ARG, "k = %lld outside [1, 2^20]", (long long)k);
   if (group < 32 || group % 32 != 0 || k % group != 0)
     return fail(CP_ERR_UNSUPPORTED, "group = %lld must be a multiple of 32 that divides k = %lld", (long long)group, (long long)k);
   if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
@@ -690,6 +690,8 @@ cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_s
   p.n = n;
   p.k = int(k);
   p.group = int(group);
+  p.group_magic = group == 32 ? 0u : unsigned(((int64_t(1) << 32) + group / 32 - 1) / (group / 32));
+  p.group_one = group == 32;
   serve_type(dtype, &p.type);
   serve_type(y_dtype, &p.y_type);
   hipError_t e = cp::launch_w4_matvec(p, static_cast<hipStream_t>(stream));

@@ -8,20 +8,22 @@
 // group come from the same instruction with a matrix of ones.  All sums are
 // float32.
 //
-// A wave works on 16 outputs (the rows of A) and MT times 16 rows of x (the
-// columns of B); the block's waves share the outputs and take runs of 128 k
-// in turn, and their sums meet in LDS.  A lane loads 16 bytes of one output's
-// codes, 32 k: where groups are multiples of 128 that is how the products take
-// them (lane group g holds k = 32 g + 8 j at step j); smaller groups need each
-// step's 32 k from one group, so the four lane groups exchange their words
-// first (k = 32 j + 8 g).
+// A lane loads 16 bytes of one output's codes, 32 k: where groups are multiples
+// of 128 that is how the products take them (lane group g holds k = 32 g + 8 j
+// at step j); smaller groups need each step's 32 k from one group, so the four
+// lane groups exchange their words first (k = 32 j + 8 g).
+//
+// Two kernels.  Few rows or outputs: a wave works on 16 outputs and 16 rows,
+// the block's waves take runs of 128 k in turn and their sums meet in LDS.
+// More rows: see w4_wide_kernel.
+#include <algorithm>
+#include <type_traits>
+
 #include "launch.h"
 #include "serve.h"
 
 namespace cp {
 namespace {
-
-constexpr int kWaves = 4;
 
 // a[d] of lane group r <-> a[r] of lane group d.
 __device__ __forceinline__ void transpose4(uint32_t* a) {
@@ -52,104 +54,422 @@ __device__ __forceinline__ u32x4 order(u32x4 w) {
   return u32x4{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
                __builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
 }
-template <class T, bool X8>
-__device__ __forceinline__ u32x4 load_x(const void* x, int64_t i) {
-  if constexpr (X8) {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + i);
-    const uint32_t even = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u), odd = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
-    return u32x4{widen2<T, false>(even), widen2<T, true>(even), widen2<T, false>(odd), widen2<T, true>(odd)};
-  } else {
-    return order<T>(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + i));
+// Eight x as they are stored, and as the operand.
+template <bool X8>
+struct RawX {
+  u32x4 w;
+  __device__ __forceinline__ void load(const uint8_t* x, unsigned element) {
+    if constexpr (X8) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(x + element);
+      w[0] = v[0];
+      w[1] = v[1];
+    } else {
+      w = *reinterpret_cast<const u32x4*>(x + 2 * element);
+    }
   }
+  // Zero where !inside: the codes that meet it are another k's.
+  template <class T>
+  __device__ __forceinline__ u32x4 operand(bool inside = true) const {
+    u32x4 r;
+    if constexpr (X8) {
+      const uint32_t even = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u), odd = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
+      r = u32x4{widen2<T, false>(even), widen2<T, true>(even), widen2<T, false>(odd), widen2<T, true>(odd)};
+    } else {
+      r = order<T>(w);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = inside ? r[e] : 0u;
+    return r;
+  }
+};
+
+// The loads above stay above: the compiler would move a load that the next
+// turn of a loop uses to where it uses it.
+__device__ __forceinline__ void keep_loads_here() { asm volatile("" ::: "memory"); }
+
+// A barrier for data in LDS only, so that loads from memory stay under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <class T>
-__device__ __forceinline__ uint32_t one2() { return pack2<T>(1.f, 1.f); }
+// SPAN: steps of 32 k between two groups' ends, 4, 2 or 1 (group a multiple of
+// 128, of 64, of 32).
+//
+// A lane's loads are never conditional: past the end of x, of the rows or of k
+// they read the last ones again, so that the next run's are under way while
+// this one's are used.  Results of rows and outputs that do not exist are not
+// stored, and x is zero past k.  Addresses are a wave's base plus 32 bits of a
+// lane's own; what is loaded stays as it is stored until it is used.
 
-template <class T, bool X8, bool SMALL, int MT>
-__global__ __launch_bounds__(64 * kWaves) void w4_kernel(W4Params p) {
-  __shared__ float s_part[kWaves][MT][16][17];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int c = lane % 16, g = lane / 16;
-  const int64_t n0 = int64_t(blockIdx.x) * 16, m0 = int64_t(blockIdx.y) * (16 * MT);
-  const int groups = p.k / p.group;
-  const int64_t row = n0 + c < p.n ? n0 + c : p.n - 1;
-  const uint8_t* wrow = p.weight + row * (p.k / 2);
-  const u32x4 ones = {one2<T>(), one2<T>(), one2<T>(), one2<T>()};
-  f32x4 y[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+// r-th run of 32 k -> its group.
+__device__ __forceinline__ int group_of(const W4Params& p, int r) {
+  return int(unsigned((uint64_t(r) * p.group_magic) >> 32) + unsigned(r) * p.group_one);
+}
 
-  for (int kb = wave * 128; kb < p.k; kb += kWaves * 128) {
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (kb + g * 32 < p.k) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(wrow + (kb + g * 32) / 2);
+// The scales and zero points of a lane's output at a run of 128 k.
+template <class T, int SPAN>
+struct Scales {
+  static constexpr int kGroups = 4 / SPAN;
+  uint16_t s[kGroups];
+  uint8_t z[kGroups];
+
+  // lane: the output's first group, from the block's first output's on.
+  __device__ __forceinline__ void load(const W4Params& p, int64_t n0, unsigned lane, int groups, int kb) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = v[j];
-    }
-    if constexpr (SMALL) transpose4(w);
-    f32x4 acc[MT], sum[MT];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (SMALL && kb + j * 32 >= p.k) break;
-      if (SMALL || j == 0) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      const u32x4 a = codes<T>(w[j]);
-      const int k = kb + (SMALL ? j * 32 + g * 8 : g * 32 + j * 8);
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const int64_t i = m0 + t * 16 + c;
-        u32x4 b = {0, 0, 0, 0};
-        if (i < p.m) b = load_x<T, X8>(p.x, i * p.k + k);
-        acc[t] = mfma32<T>(a, b, acc[t]);
-        sum[t] = mfma32<T>(ones, b, sum[t]);
-      }
-      if (SMALL || j == 3) {
-        const int group = (kb + (SMALL ? j * 32 : 0)) / p.group;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t nr = n0 + g * 4 + r < p.n ? n0 + g * 4 + r : p.n - 1;
-          const float s = load1<T>(p.scale, nr * groups + group);
-          const float z = p.zero ? float(p.zero[nr * groups + group]) : 8.f;
-#pragma unroll
-          for (int t = 0; t < MT; ++t) y[t][r] = fmaf(s, fmaf(512.f, acc[t][r], -z * sum[t][r]), y[t][r]);
-        }
-      }
+    for (int j = 0; j < kGroups; ++j) {
+      const int64_t base = n0 * groups + min(group_of(p, kb / 32 + j * SPAN), groups - 1);
+      s[j] = (static_cast<const uint16_t*>(p.scale) + base)[lane];
+      // Without zero points a byte of the scales is read in their place and dropped.
+      z[j] = ((p.zero ? p.zero : static_cast<const uint8_t*>(p.scale)) + base)[lane];
     }
   }
+  __device__ __forceinline__ float scale(int j) const { return unpack2<T>(s[j]).x; }
+  __device__ __forceinline__ float zero(const W4Params& p, int j) const { return p.zero ? float(z[j]) : 8.f; }
+};
 
+// The 32 codes of lane group g at a run of 128 k; lane: the output's first byte.
+__device__ __forceinline__ u32x4 load_codes(const W4Params& p, int64_t n0, unsigned lane, int kb, int g) {
+  const int last = (p.k - 1) / 128 * 128, at = min(kb, last);
+  const uint8_t* base = p.weight + n0 * (p.k / 2) + at / 2;
+  return *reinterpret_cast<const u32x4*>(base + (lane + unsigned(min(g * 32, p.k - 32 - at)) / 2));
+}
+
+template <class T, int SPAN>
+__device__ __forceinline__ void operands(u32x4 w, u32x4* a) {
+  uint32_t v[4] = {w[0], w[1], w[2], w[3]};
+  if constexpr (SPAN < 4) transpose4(v);
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int j = 0; j < 4; ++j) a[j] = codes<T>(v[j]);
+}
+
+// Up to 16 rows.  A wave works on 16 RT outputs, whose x it reads from the
+// caches and puts in order once for all of them, at every waves-th run of 128
+// k; the sums of the block's waves meet in LDS.
+template <class T, bool X8, int SPAN, int RT>
+__global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
+  constexpr int kGroups = 4 / SPAN;
+  extern __shared__ float s_part[];               // [waves][RT][16][17]
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
+  const int c = lane % 16, g = lane / 16;
+  const int64_t n0 = int64_t(blockIdx.x) * (16 * RT), m0 = int64_t(blockIdx.y) * 16;
+  const int groups = p.k / p.group;
+  const uint32_t one = pack2<T>(1.f, 1.f);
+  const u32x4 ones = {one, one, one, one};
+  unsigned row[RT];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s_part[wave][t][c][g * 4 + r] = y[t][r];
+  for (int i = 0; i < RT; ++i) row[i] = unsigned(min(int64_t(i * 16 + c), p.n - 1 - n0));
+  const unsigned xrow = unsigned(min(int64_t(c), p.m - 1 - m0)) * unsigned(p.k);
+  const uint8_t* xbase = static_cast<const uint8_t*>(p.x) + m0 * p.k * (X8 ? 1 : 2);
+  f32x4 y[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto k_of = [&](int kb, int j) { return kb + (SPAN < 4 ? j * 32 + g * 8 : g * 32 + j * 8); };
+  struct Stage {
+    u32x4 w[RT];
+    Scales<T, SPAN> sc[RT];
+    RawX<X8> x[4];
+  } stage;
+  // What a run needs, on its way while the run before is worked on.
+  auto load = [&](Stage& s, int kb) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) s.w[i] = load_codes(p, n0, row[i] * unsigned(p.k / 2), kb, g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_of(kb, j), p.k - 8)));
+#pragma unroll
+    for (int i = 0; i < RT; ++i) s.sc[i].load(p, n0, row[i] * unsigned(groups), groups, kb);
+    keep_loads_here();
+  };
+  const int step = waves * 128;
+  auto use = [&](auto more, Stage& s, int kb) {
+    u32x4 a[RT][4], b[4];
+    float sc[RT][kGroups], z[RT][kGroups];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = s.x[j].template operand<T>(SPAN == 4 || k_of(kb, j) < p.k);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      operands<T, SPAN>(s.w[i], a[i]);
+#pragma unroll
+      for (int h = 0; h < kGroups; ++h) {
+        sc[i][h] = 512.f * s.sc[i].scale(h);
+        z[i][h] = -s.sc[i].scale(h) * s.sc[i].zero(p, h);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more || kb + step < p.k) load(s, kb + step);
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f}, acc[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = h * SPAN; j < (h + 1) * SPAN; ++j) {
+        sum = mfma32<T>(b[j], ones, sum);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[i] = mfma32<T>(b[j], a[i][j], acc[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[i][r] = fmaf(sc[i][h], acc[i][r], fmaf(z[i][h], sum[r], y[i][r]));
+    }
+  };
+  int kb = wave * 128;
+  load(stage, kb);
+  for (; kb + step < p.k; kb += step) use(std::true_type(), stage, kb);
+  if (kb < p.k) use(std::false_type(), stage, kb);
+
+  // y[i][r] of lane (g, c): output 16 i + c of row 4 g + r.
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_part[((wave * RT + i) * 16 + g * 4 + r) * 17 + c] = y[i][r];
   __syncthreads();
-  for (int i = threadIdx.x; i < MT * 256; i += 64 * kWaves) {
-    const int t = i / 256, mr = (i / 16) % 16, nr = i % 16;
-    const int64_t m = m0 + t * 16 + mr, n = n0 + nr;
+  for (int e = threadIdx.x; e < RT * 256; e += blockDim.x) {
+    const int i = e / 16 % RT, mr = e / (16 * RT);
+    const int64_t m = m0 + mr, n = n0 + i * 16 + e % 16;
     if (m >= p.m || n >= p.n) continue;
     float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += s_part[w][t][mr][nr];
+    for (int x = 0; x < waves; ++x) v += s_part[((x * RT + i) * 16 + mr) * 17 + e % 16];
     if (X8) v *= p.x_scale[m];
     if (p.y_type == ServeType::kF32) store1<F32>(p.y, m * p.n + n, v);
     else store1<T>(p.y, m * p.n + n, v);
   }
 }
 
-template <class T, bool X8, bool SMALL, int MT>
-hipError_t launch(const W4Params& p, hipStream_t stream) {
-  const dim3 grid(unsigned((p.n + 15) / 16), unsigned((p.m + 16 * MT - 1) / (16 * MT)));
-  w4_kernel<T, X8, SMALL, MT><<<grid, dim3(64 * kWaves), 0, stream>>>(p);
+// Scales and zero points go to LDS some groups at a time: a lane needs those
+// of one output, so its own loads would touch a cache line each, as many as
+// its codes do.  Row o of `rows` outputs from n0 on, groups g0 .. g0 + count - 1.
+template <int PITCH>
+__device__ __forceinline__ void keep_scales(const W4Params& p, int64_t n0, int rows, int g0, int count, uint16_t* s, uint8_t* z) {
+  const int groups = p.k / p.group, last = int(min(int64_t(rows), p.n - n0)) - 1;
+  for (int i = threadIdx.x % kWave; i < count; i += kWave) {
+#pragma unroll 4
+    for (int o = threadIdx.x / kWave; o < rows; o += blockDim.x / kWave) {
+      const int64_t at = (n0 + min(o, last)) * groups + g0 + i;
+      s[o * PITCH + i] = static_cast<const uint16_t*>(p.scale)[at];
+      z[o * PITCH + i] = p.zero ? p.zero[at] : uint8_t(8);
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ float widen1(uint16_t bits) { return unpack2<T>(bits).x; }
+
+// Sum over the 4, 8 or 16 neighbouring lanes that hold 32 SPAN k; they all get it.
+template <int SPAN>
+__device__ __forceinline__ float span_sum(float x) {
+  auto moved = [](float v, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  x += moved(x, std::integral_constant<int, 0xb1>());                      // quad: 1 0 3 2
+  x += moved(x, std::integral_constant<int, 0x4e>());                      // quad: 2 3 0 1
+  if constexpr (SPAN >= 2) x += moved(x, std::integral_constant<int, 0x141>());   // half rows reversed
+  if constexpr (SPAN >= 4) x += moved(x, std::integral_constant<int, 0x140>());   // rows reversed
+  return x;
+}
+
+// c + the two products of a packed pair of T with 1.
+template <class T>
+__device__ __forceinline__ float add2(uint32_t w, float c);
+template <>
+__device__ __forceinline__ float add2<Bf16>(uint32_t w, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
+}
+template <>
+__device__ __forceinline__ float add2<F16>(uint32_t w, float c) {
+  return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), f16x2{(_Float16)1.f, (_Float16)1.f}, c, false);
+}
+
+// 16 MT rows of x by 128 outputs.  x would be read once per 16 outputs from the
+// caches if each wave did so by itself, many times the weights' bytes; here
+// the block brings 256 k of it to LDS at a time, as operands, with the groups'
+// sums beside them, while it works on the 256 before.  Waves: 8 by outputs (16
+// each) times 2 by k; codes are loaded two turns ahead.
+constexpr int kWideRows = 128;
+constexpr int kWideGroups = 64;                   // whose scales are in LDS at a time
+template <class T, bool X8, int SPAN, int MT>
+__global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
+  constexpr int kGroups = 4 / SPAN, kPitch = kWideGroups + 2, kMine = MT / 2;
+  __shared__ u32x4 s_x[2][2][4][MT][kWave];       // [turn % 2][half][step][row tile][lane]
+  __shared__ uint16_t s_scale[kWideRows * kPitch];
+  __shared__ uint8_t s_zero[kWideRows * kPitch];
+  __shared__ float s_sum[2][2][MT][kWave];        // [turn % 2][half][row tile][group, row]
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int c = lane % 16, g = lane / 16, half = wave / 8;
+  const int64_t first = int64_t(blockIdx.x) * kWideRows, out0 = first + wave % 8 * 16, n0 = min(out0, p.n - 1);
+  const int64_t m0 = int64_t(blockIdx.y) * (16 * MT);
+  const int turns = (p.k + 255) / 256, last_group = p.k / p.group - 1;
+  const unsigned row = unsigned(min(int64_t(c), p.n - 1 - n0)) * unsigned(p.k / 2);
+  f32x4 y[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // This thread's share of a turn's x: 8 k from 8 q on of a half, row xr of
+  // every other tile.  A wave holds four rows' 128 k, whose operands would
+  // fall into the same banks; so the rows of a step's lane group change places.
+  const int q = tid % 16, xhalf = wave / 4 % 2, xr = tid / 16 % 16, xt = wave / 8, xk = xhalf * 128 + q * 8;
+  const int xj = SPAN < 4 ? q / 4 : q % 4, xg = SPAN < 4 ? q % 4 : q / 4;
+  const int slot = xg * 16 + (xr ^ (xj * 4 + xg));
+  const uint8_t* xbase = static_cast<const uint8_t*>(p.x) + m0 * p.k * (X8 ? 1 : 2);
+  unsigned xrow[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) xrow[i] = unsigned(min(int64_t((2 * i + xt) * 16 + xr), p.m - 1 - m0)) * unsigned(p.k);
+  // Groups past a run's last are multiplied by zero.
+  for (int i = tid; i < 2 * 2 * MT * kWave; i += 1024) (&s_sum[0][0][0][0])[i] = 0.f;
+  __syncthreads();
+  RawX<X8> xv[2][kMine];
+  u32x4 w[2];
+  auto load_x = [&](RawX<X8>* v, int turn) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) v[i].load(xbase, xrow[i] + unsigned(min(turn * 256 + xk, p.k - 8)));
+    keep_loads_here();
+  };
+  auto load_w = [&](u32x4* v, int turn) {
+    *v = load_codes(p, n0, row, turn * 256 + half * 128, g);
+    keep_loads_here();
+  };
+  auto keep_x = [&](auto whole, const RawX<X8>* raw, int buf, int turn) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      u32x4 v = raw[i].template operand<T>(whole || turn * 256 + xk < p.k);
+      s_x[buf][xhalf][xj][2 * i + xt][slot] = v;
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = add2<T>(v[e], s);
+      s = span_sum<SPAN>(s);
+      if (q % (4 * SPAN) == 0) s_sum[buf][xhalf][2 * i + xt][q / (4 * SPAN) * 16 + xr] = s;
+    }
+  };
+  int g0 = 0;                                     // first group whose scales are in LDS
+  // One turn: its x is in s_x[buf], its codes in w[buf]; the turn after's x is
+  // in xv[1 - buf] or on its way.
+  auto turn_of = [&](auto more, int buf, int turn) {
+    float scale[kGroups], zero = 0.f;             // lane group g gives the zero points of the run's group g
+    uint32_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = w[buf][j];
+    if constexpr (SPAN < 4) transpose4(v);
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+      const int at = (wave % 8 * 16 + c) * kPitch + min(group_of(p, turn * 8 + half * 4 + h * SPAN), last_group) - g0;
+      const float s = widen1<T>(s_scale[at]);
+      scale[h] = 512.f * s;
+      zero = g == h ? -s * float(s_zero[at]) : zero;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more || turn + 2 < turns) {
+      // x first: what waits for it, at the end of the next turn, then does not
+      // wait for the codes of the turn after.
+      load_x(xv[buf], turn + 2);
+      load_w(&w[buf], turn + 2);
+    }
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+      f32x4 acc[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = h * SPAN; j < (h + 1) * SPAN; ++j) {
+        const u32x4 a = codes<T>(v[j]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = mfma32<T>(s_x[buf][half][j][t][g * 16 + (c ^ (j * 4 + g))], a, acc[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[t][r] = fmaf(scale[h], acc[t][r], y[t][r]);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) y[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(s_sum[buf][half][t][g * 16 + c], zero, y[t], 0, 0, 0);
+    if (more || turn + 1 < turns) keep_x(more, xv[1 - buf], 1 - buf, turn + 1);
+    lds_barrier();
+  };
+  load_x(xv[0], 0);
+  load_w(&w[0], 0);
+  load_x(xv[1], 1);
+  load_w(&w[1], 1);
+  keep_x(std::false_type(), xv[0], 0, 0);
+  lds_barrier();
+  // kWideGroups groups are `block` turns, an even number (group / 4).  While two
+  // more turns are certain nothing about the loads is conditional, so that
+  // each wait is for just what it needs.
+  const int block = kWideGroups * p.group / 256;
+  for (int turn = 0; turn < turns;) {
+    const int stop = min(turn + block, turns);
+    g0 = group_of(p, turn * 8);
+    keep_scales<kPitch>(p, first, kWideRows, g0, min(kWideGroups, last_group + 1 - g0), s_scale, s_zero);
+    lds_barrier();
+    for (; turn + 4 <= turns && turn < stop; turn += 2) {
+      turn_of(std::true_type(), 0, turn);
+      turn_of(std::true_type(), 1, turn + 1);
+    }
+    for (; turn < stop; turn += 2) {
+      turn_of(std::false_type(), 0, turn);
+      if (turn + 1 < turns) turn_of(std::false_type(), 1, turn + 1);
+    }
+  }
+
+  // The halves meet.  y[t][r] of lane (g, c): output c of row 16 t + 4 g + r.
+  f32x4* part = &reinterpret_cast<f32x4*>(&s_x[0][0][0][0][0])[wave % 8 * (MT * kWave) + lane];
+  if (half == 1)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) part[t * kWave] = y[t];
+  __syncthreads();
+  if (half == 1) return;
+  const int64_t n = out0 + c;
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const f32x4 o = part[t * kWave];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = m0 + t * 16 + g * 4 + r;
+      if (m >= p.m || n >= p.n) continue;
+      float v = y[t][r] + o[r];
+      if (X8) v *= p.x_scale[m];
+      if (p.y_type == ServeType::kF32) store1<F32>(p.y, m * p.n + n, v);
+      else store1<T>(p.y, m * p.n + n, v);
+    }
+  }
+}
+
+template <class T, bool X8, int SPAN, int MT>
+hipError_t launch_wide(const W4Params& p, hipStream_t stream) {
+  const dim3 grid(unsigned((p.n + kWideRows - 1) / kWideRows), unsigned((p.m + 16 * MT - 1) / (16 * MT)));
+  w4_wide_kernel<T, X8, SPAN, MT><<<grid, dim3(1024), 0, stream>>>(p);
   return hipGetLastError();
+}
+
+template <class T, bool X8, int SPAN, int RT>
+hipError_t launch_few(const W4Params& p, hipStream_t stream) {
+  const int waves = std::min(RT == 4 ? 4 : 8, (p.k + 127) / 128);
+  const dim3 grid(unsigned((p.n + 16 * RT - 1) / (16 * RT)), unsigned((p.m + 15) / 16));
+  w4_few_kernel<T, X8, SPAN, RT><<<grid, dim3(kWave * waves), size_t(waves) * RT * 272 * sizeof(float), stream>>>(p);
+  return hipGetLastError();
+}
+
+// Which kernel (times of one call in a graph, k = 3584, groups of 128, us):
+//   - more than 16 rows and many outputs: the wide one, whose time hardly
+//     depends on n up to a block a compute unit (64 rows: 29 at n = 4608, 30 at
+//     28672; 32 rows: 22 at 28672), while that of the other grows with it (64
+//     rows: 19 and 58; 32 rows: 12 and 35);
+//   - otherwise 16 outputs a wave while there are fewer than two waves' worth a
+//     compute unit (one row, n = 1500: 3.8 against 5.3 with 32; n = 4608: 6.4
+//     against 5.7), 64 when there are plenty (16 rows, n = 28672: 27 against
+//     30; one row 14.8 against 15.8; but one row, n = 4608 10.1).
+template <class T, bool X8, int SPAN>
+hipError_t launch_span(const W4Params& p, hipStream_t stream) {
+  if (p.m > 16 && p.n >= (p.m > 32 ? 8192 : 10240))
+    return p.m <= 32 ? launch_wide<T, X8, SPAN, 2>(p, stream) : launch_wide<T, X8, SPAN, 4>(p, stream);
+  const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
+  if (tiles >= 1024) return launch_few<T, X8, SPAN, 4>(p, stream);
+  return tiles >= 256 ? launch_few<T, X8, SPAN, 2>(p, stream) : launch_few<T, X8, SPAN, 1>(p, stream);
 }
 
 template <class T, bool X8>
 hipError_t launch_type(const W4Params& p, hipStream_t stream) {
-  const bool small = p.group % 128 != 0;
-  if (p.m <= 16) return small ? launch<T, X8, true, 1>(p, stream) : launch<T, X8, false, 1>(p, stream);
-  return small ? launch<T, X8, true, 4>(p, stream) : launch<T, X8, false, 4>(p, stream);
+  if (p.group % 128 == 0) return launch_span<T, X8, 4>(p, stream);
+  if (p.group % 64 == 0) return launch_span<T, X8, 2>(p, stream);
+  return launch_span<T, X8, 1>(p, stream);
 }
 
 }  // namespace

@@ -222,7 +222,9 @@ struct W4Params {
   const uint8_t* zero;            // [n, k / group] or nullptr (8)
   void* y;                        // [m, n]
   int64_t m, n;
-  int k, group;                   // k % group == 0, group % 32 == 0
+  int k, group;                   // k % group == 0, group % 32 == 0, k <= 2^20
+  unsigned group_magic;           // r / (group / 32) = (r * magic >> 32) + r * one for r <= 2^15:
+  unsigned group_one;             // magic = ceil(2^32 / (group / 32)) and one = 0, or for group 32 0 and 1
   ServeType type;                 // kBf16 or kF16
   ServeType y_type;               // `type` or kF32
 };

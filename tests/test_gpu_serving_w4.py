@@ -39,7 +39,10 @@ def _check(x, w, s, z, xs, out_dtype=None):
     (1, 1, 32, 32), (1, 16, 64, 32), (2, 33, 96, 96), (3, 15, 160, 32), (1, 128, 128, 128), (7, 48, 384, 128),
     (15, 17, 256, 256), (16, 100, 192, 64), (17, 64, 512, 128), (5, 1500, 1184, 32), (33, 130, 640, 64),
     (64, 257, 1024, 128), (65, 96, 320, 160), (130, 40, 896, 128), (1, 4608, 3584, 128), (4, 70, 4480, 4480),
-    (9, 96, 2112, 96), (24, 300, 7168, 256)])
+    (9, 96, 2112, 96), (24, 300, 7168, 256),
+    # many outputs: 64 a wave; and, with more than 16 rows, x shared in LDS
+    (1, 16400, 256, 128), (6, 16390, 416, 32), (16, 4200, 576, 64), (17, 10250, 384, 128), (20, 10241, 160, 32),
+    (33, 8200, 320, 32), (64, 8192, 1088, 64), (130, 8300, 2208, 96), (40, 8195, 2304, 32), (64, 8321, 256, 256)])
 def test_products(m, n, k, group, t, x8):
     zero = (m + n) % 2 == 1
     print(f"w4 m={m} n={n} k={k} group={group} {t} x8={x8} zero={zero}", flush=True)
@@ -67,10 +70,11 @@ def test_no_rows():
     assert cp.w4_matvec(x, w, s, zero=z).shape == (0, 32)
 
 
-def test_rows_do_not_touch_each_other():
+@pytest.mark.parametrize("n", [100, 10300])
+def test_rows_do_not_touch_each_other(n):
     """NaN or infinity in one row of x reaches that row's results only."""
     import paper_2608_13226_amd as cp
-    x, w, s, z, _ = _data(20, 100, 512, 128, BF, False, True)
+    x, w, s, z, _ = _data(20, n, 512, 128, BF, False, True)
     clean = cp.w4_matvec(x, w, s, zero=z)
     x[3, 7], x[18, 500] = float("nan"), float("inf")
     y = cp.w4_matvec(x, w, s, zero=z)

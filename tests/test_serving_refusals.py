@@ -50,7 +50,7 @@ def _w4(lib, **kw):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(m=-1), INVALID), (dict(m=(1 << 20) + 1), INVALID), (dict(n=0), INVALID), (dict(n=1 << 31), INVALID), (dict(k=0), INVALID),
-    (dict(k=1 << 31), INVALID), (dict(group=0), UNSUPPORTED), (dict(group=16), UNSUPPORTED), (dict(group=48), UNSUPPORTED),
+    (dict(k=(1 << 20) + 32), INVALID), (dict(group=0), UNSUPPORTED), (dict(group=16), UNSUPPORTED), (dict(group=48), UNSUPPORTED),
     (dict(group=96), UNSUPPORTED), (dict(dtype=F32), UNSUPPORTED), (dict(x_dtype=F16), UNSUPPORTED), (dict(y_dtype=F16), UNSUPPORTED),
     (dict(y_dtype=E4M3), UNSUPPORTED), (dict(x_scale=FAKE), INVALID), (dict(x_dtype=E4M3), INVALID), (dict(x=None), INVALID),
     (dict(weight=None), INVALID), (dict(scale=None), INVALID), (dict(y=None), INVALID), (dict(x=ODD), INVALID),
