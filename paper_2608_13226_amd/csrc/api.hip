@@ -820,6 +820,9 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
   p.d = int(d);
   p.page = int(page_size);
   p.width = int(width);
+  p.page_shift = 0;
+  while ((int64_t(1) << p.page_shift) < page_size) ++p.page_shift;
+  p.page_magic = unsigned(((int64_t(1) << (31 + p.page_shift)) + page_size - 1) / page_size);
   p.window = int(std::min<int64_t>(window, max_length));
   p.scale = scale;
   p.cache8 = cache_dtype == CP_E4M3;

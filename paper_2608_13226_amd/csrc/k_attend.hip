@@ -20,6 +20,7 @@
 // p is handed over as two values of the cache's type (its rounding and the
 // rest), so no accuracy is lost to it; sums and statistics are float32.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "serve.h"
@@ -27,7 +28,6 @@
 namespace cp {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kTile = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -40,77 +40,133 @@ template <int D>
 struct Dims {
   static constexpr int n8 = D / 128, n4 = D % 128 / 64, n2 = D % 64 / 32;
   static constexpr int pairs = D / 32;          // packed pairs a lane holds of a token
-  // First dim of pair q of lane c.
-  static __device__ __forceinline__ int dim(int q, int c) {
-    if (q < 4 * n8) return q / 4 * 128 + c * 8 + q % 4 * 2;
-    if (q < 4 * n8 + 2 * n4) return n8 * 128 + c * 4 + (q - 4 * n8) * 2;
-    return n8 * 128 + n4 * 64 + c * 2;
+};
+
+// A lane's dims of one token's value row, as they are stored, and as packed pairs of T.
+template <class T, bool C8, int D>
+struct RawValue {
+  using L = Dims<D>;
+  static constexpr int kWords = C8 ? (L::pairs + 1) / 2 : L::pairs;
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ void load(const uint8_t* row, int c) {
+    constexpr int kB = C8 ? 1 : 2;
+#pragma unroll
+    for (int i = 0; i < L::n8; ++i) {
+      if constexpr (C8) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(row + i * 128 + c * 8);
+        w[2 * i] = v[0];
+        w[2 * i + 1] = v[1];
+      } else {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(row + i * 256 + c * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+      }
+    }
+    const uint8_t* rest = row + L::n8 * 128 * kB;
+    constexpr int at = L::n8 * (C8 ? 2 : 4);
+    if constexpr (L::n4) {
+      if constexpr (C8) {
+        w[at] = *reinterpret_cast<const uint32_t*>(rest + c * 4);
+      } else {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(rest + c * 8);
+        w[at] = v[0];
+        w[at + 1] = v[1];
+      }
+    }
+    if constexpr (L::n2) {
+      const uint8_t* last = rest + L::n4 * 64 * kB;
+      if constexpr (C8) w[at + L::n4] = *reinterpret_cast<const uint16_t*>(last + c * 2);
+      else w[at + 2 * L::n4] = *reinterpret_cast<const uint32_t*>(last + c * 4);
+    }
+  }
+  // Packed pair q.
+  __device__ __forceinline__ uint32_t pair(int q) const {
+    if constexpr (!C8) return w[q];
+    return q % 2 == 0 ? widen2<T, false>(w[q / 2]) : widen2<T, true>(w[q / 2]);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
   }
 };
 
-// A lane's dims of one token's value row, as packed pairs of T.
+// The dims of step j that lane group g takes of a key and of the query, and
+// how a key's are loaded: eight at a time (16 bytes), or with 8-bit caches
+// sixteen, for two steps.
+template <bool C8, int D>
+__device__ __forceinline__ int key_dim(int j, int g) {
+  if (C8 && j / 2 * 64 + 64 <= D) return j / 2 * 64 + g * 16 + j % 2 * 8;
+  return j * 32 + g * 8;
+}
 template <class T, bool C8, int D>
-__device__ __forceinline__ void load_value(const uint8_t* row, int c, uint32_t* out) {
-  using L = Dims<D>;
-  if constexpr (!C8) {
+struct RawKey {
+  static constexpr int kSteps = D / 32;
+  u32x4 w[C8 ? (kSteps + 1) / 2 : kSteps];
+
+  // row: the token's row, past the lane group's first dims (16 g bytes, or 8 g
+  // where the last step is alone).
+  __device__ __forceinline__ void load(const uint8_t* row, int g) {
+    if constexpr (!C8) {
 #pragma unroll
-    for (int i = 0; i < L::n8; ++i) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(row + i * 256 + c * 16);
+      for (int j = 0; j < kSteps; ++j) w[j] = *reinterpret_cast<const u32x4*>(row + j * 64 + g * 16);
+    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) out[4 * i + j] = w[j];
-    }
-    if constexpr (L::n4) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(row + L::n8 * 256 + c * 8);
-      out[4 * L::n8] = w[0];
-      out[4 * L::n8 + 1] = w[1];
-    }
-    if constexpr (L::n2) out[4 * L::n8 + 2 * L::n4] = *reinterpret_cast<const uint32_t*>(row + L::n8 * 256 + L::n4 * 128 + c * 4);
-  } else {
-#pragma unroll
-    for (int i = 0; i < L::n8; ++i) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(row + i * 128 + c * 8);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        out[4 * i + 2 * j] = widen2<T, false>(w[j]);
-        out[4 * i + 2 * j + 1] = widen2<T, true>(w[j]);
+      for (int j = 0; j < kSteps / 2; ++j) w[j] = *reinterpret_cast<const u32x4*>(row + j * 64 + g * 16);
+      if constexpr (kSteps % 2) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(row + kSteps / 2 * 64 + g * 8);
+        w[kSteps / 2][0] = v[0];
+        w[kSteps / 2][1] = v[1];
       }
     }
-    if constexpr (L::n4) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(row + L::n8 * 128 + c * 4);
-      out[4 * L::n8] = widen2<T, false>(w);
-      out[4 * L::n8 + 1] = widen2<T, true>(w);
-    }
-    if constexpr (L::n2)
-      out[4 * L::n8 + 2 * L::n4] = widen2<T, false>(*reinterpret_cast<const uint16_t*>(row + L::n8 * 128 + L::n4 * 64 + c * 2));
   }
+  __device__ __forceinline__ u32x4 step(int j) const {
+    if constexpr (!C8) return w[j];
+    const uint32_t a = w[j / 2][j % 2 * 2], b = w[j / 2][j % 2 * 2 + 1];
+    return u32x4{widen2<T, false>(a), widen2<T, true>(a), widen2<T, false>(b), widen2<T, true>(b)};
+  }
+};
+
+// p as two values of T: one near it, and the rest.
+template <class T>
+__device__ __forceinline__ void split2(float a, float b, uint32_t& near, uint32_t& rest);
+template <>
+__device__ __forceinline__ void split2<Bf16>(float a, float b, uint32_t& near, uint32_t& rest) {
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  near = __builtin_amdgcn_perm(y, x, 0x07060302u);
+  rest = pack2<Bf16>(a - __uint_as_float(x & 0xffff0000u), b - __uint_as_float(y & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ void split2<F16>(float a, float b, uint32_t& near, uint32_t& rest) {
+  near = pack2<F16>(a, b);
+  const float2 r = unpack2<F16>(near);
+  rest = pack2<F16>(a - r.x, b - r.y);
 }
 
-// Eight dims from dim d on of one token's key row.
-template <class T, bool C8>
-__device__ __forceinline__ u32x4 load_key(const uint8_t* row, int d) {
-  if constexpr (!C8) return *reinterpret_cast<const u32x4*>(row + 2 * d);
-  const u32x2 w = *reinterpret_cast<const u32x2*>(row + d);
-  return u32x4{widen2<T, false>(w[0]), widen2<T, true>(w[0]), widen2<T, false>(w[1]), widen2<T, true>(w[1])};
-}
+// Loads above stay above: the compiler would move a load that the next turn of
+// a loop uses to where it uses it.
+__device__ __forceinline__ void keep_loads_here() { asm volatile("" ::: "memory"); }
 
 // One (sequence, key-value head, up to 16 of its query heads, run of tiles).
 // Partial results of run s: o [head][D], then m and l, unnormalised.
-template <class T, bool C8, int D>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
-                                                             float* part_ml) {
+// UNI: pages are multiples of a tile, so a tile's tokens follow each other in
+// memory and its address is the wave's; otherwise each lane finds one token's
+// row and the lanes exchange them.
+template <class T, bool C8, int D, int W, bool UNI>
+__global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
+                                                           float* part_ml) {
   constexpr int kSteps = D / 32;
   using L = Dims<D>;
-  __shared__ float s_o[kWaves][16][D + 4];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  __shared__ float s_o[W][16][D + 4];
+  __shared__ float s_m[W][16], s_l[W][16];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16, g = lane / 16;
   const int group = p.hq / p.hk, head_tiles = (group + 15) / 16;
   const int run = blockIdx.x, kh = blockIdx.y / head_tiles, h0 = kh * group + blockIdx.y % head_tiles * 16;
   const int heads = min(16, (kh + 1) * group - h0);
   const int b = blockIdx.z;
 
-  int hi = p.lengths[b];
-  hi = max(0, int(min(int64_t(hi), p.max_length)));
+  const int hi = max(0, int(min(int64_t(__builtin_amdgcn_readfirstlane(p.lengths[b])), p.max_length)));
   const int lo = p.window > 0 ? max(0, hi - p.window) : 0;
   const int tile0 = lo / kTile + run * tiles_per_run;
   const int tile1 = min((hi + kTile - 1) / kTile, tile0 + tiles_per_run);
@@ -124,7 +180,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int
   for (int j = 0; j < kSteps; ++j) {
     q[j] = u32x4{0, 0, 0, 0};
     if (c < heads)
-      q[j] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + (int64_t(b) * p.hq + h0 + c) * D + j * 32 + g * 8);
+      q[j] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + (int64_t(b) * p.hq + h0 + c) * D + key_dim<C8, D>(j, g));
   }
   const float to_log2 = p.scale * kLog2e * (p.k_scale ? p.k_scale[kh] : 1.f);
 
@@ -133,48 +189,63 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int
 #pragma unroll
   for (int i = 0; i < 2 * L::pairs; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  for (int tile = tile0 + wave; tile < tile1; tile += kWaves) {
+  // Which token of a tile this lane looks up: one each, or the tile's first.
+  // Tokens outside [lo, hi) take the nearest one inside (their p is 0).
+  auto token = [&](int tile) { return UNI ? tile * kTile : min(max(tile * kTile + lane % 32, lo), hi - 1); };
+  auto page_index = [&](int t) { return int(__umulhi(2u * unsigned(t), p.page_magic) >> p.page_shift); };
+  auto look_up = [&](int tile) { return table[page_index(token(min(tile, tile1 - 1)))]; };
+  auto row_of = [&](int tile, int32_t entry) {
+    const int t = token(tile);
+    const unsigned page = min(unsigned(UNI ? __builtin_amdgcn_readfirstlane(entry) : entry), unsigned(p.pages - 1));
+    return (page * unsigned(p.hk) + unsigned(kh)) * unsigned(p.page) + unsigned(t - page_index(t) * p.page);
+  };
+  // Row of the tile's token i, where lanes of a group want different ones.
+  auto row = [&](unsigned mine, int i) {
+    return UNI ? uint64_t(mine) * kRow + unsigned(i) * kRow : uint64_t(unsigned(__shfl(int(mine), i))) * kRow;
+  };
+  RawKey<T, C8, D> key[2];
+  RawValue<T, C8, D> val[8];
+  auto load_keys = [&](unsigned mine) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) key[i].load(kc + row(mine, i * 16 + c), g);
+    keep_loads_here();
+  };
+  auto load_values = [&](unsigned mine) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) val[i].load(vc + row(mine, i / 4 * 16 + g * 4 + i % 4), c);
+    keep_loads_here();
+  };
+
+  // One tile.  The next one's keys are loaded as soon as this one's are used,
+  // its values likewise, the page of the one after that meanwhile: a wave has
+  // a tile under way all the time without a second set of registers.
+  int32_t entry = 0;
+  auto work = [&](auto more, int tile) {
     const int t0 = tile * kTile;
-    // Lane l finds token l % 32's row; tokens outside [lo, hi) take the
-    // nearest one inside (their p is 0, and theirs of V too).
-    const int t = min(max(t0 + lane % 32, lo), hi - 1);
-    const int pg = t / p.page;
-    const unsigned page = min(unsigned(table[pg]), unsigned(p.pages - 1));
-    const unsigned my_row = (page * unsigned(p.hk) + unsigned(kh)) * unsigned(p.page) + unsigned(t - pg * p.page);
-
-    u32x4 key[2][kSteps];
-    uint32_t val[8][L::pairs];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* r = kc + uint64_t(unsigned(__shfl(int(my_row), i * 16 + c))) * kRow;
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) key[i][j] = load_key<T, C8>(r, j * 32 + g * 8);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint8_t* r = vc + uint64_t(unsigned(__shfl(int(my_row), i / 4 * 16 + g * 4 + i % 4))) * kRow;
-      load_value<T, C8, D>(r, c, val[i]);
-    }
-
     f32x4 s[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kSteps; ++j) s[i] = mfma32<T>(key[i][j], q[j], s[i]);
+      for (int j = 0; j < kSteps; ++j) s[i] = mfma32<T>(key[i].step(j), q[j], s[i]);
     }
-    const bool partial = t0 < lo || t0 + kTile > hi;
+    unsigned next = 0;
+    if (more) {
+      next = row_of(tile + W, entry);
+      load_keys(next);
+      entry = look_up(tile + 2 * W);
+      keep_loads_here();
+    }
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4] * to_log2;
-    if (partial) {
+    if (t0 < lo || t0 + kTile > hi) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int at = t0 + i / 4 * 16 + g * 4 + i % 4;
         if (at < lo || at >= hi) {
           x[i] = -INFINITY;
-#pragma unroll
-          for (int j = 0; j < L::pairs; ++j) val[i][j] = 0;
+          val[i].clear();
         }
       }
     }
@@ -185,34 +256,47 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m2 = fmaxf(m, top);
-      const float f = m2 == m ? 1.f : exp2f(m - m2);
+      const float f = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m - m2);
       m = m2;
       l *= f;
 #pragma unroll
       for (int i = 0; i < 2 * L::pairs; ++i) o[i] *= f;
     }
-    u32x4 ph, pl;
+    u32x4 near, rest;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float a = exp2f(x[i] - m), e = exp2f(x[i + 1] - m);
+      const float a = __builtin_amdgcn_exp2f(x[i] - m), e = __builtin_amdgcn_exp2f(x[i + 1] - m);
       l += a + e;
-      ph[i / 2] = pack2<T>(a, e);
-      const float2 r = unpack2<T>(ph[i / 2]);
-      pl[i / 2] = pack2<T>(a - r.x, e - r.y);
+      uint32_t n2, r2;
+      split2<T>(a, e, n2, r2);
+      near[i / 2] = n2;
+      rest[i / 2] = r2;
     }
 #pragma unroll
     for (int i = 0; i < L::pairs; ++i) {
       u32x4 even, odd;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        even[j] = __builtin_amdgcn_perm(val[2 * j + 1][i], val[2 * j][i], 0x05040100u);
-        odd[j] = __builtin_amdgcn_perm(val[2 * j + 1][i], val[2 * j][i], 0x07060302u);
+        const uint32_t a = val[2 * j].pair(i), e = val[2 * j + 1].pair(i);
+        even[j] = __builtin_amdgcn_perm(e, a, 0x05040100u);
+        odd[j] = __builtin_amdgcn_perm(e, a, 0x07060302u);
       }
-      o[2 * i] = mfma32<T>(even, ph, o[2 * i]);
-      o[2 * i] = mfma32<T>(even, pl, o[2 * i]);
-      o[2 * i + 1] = mfma32<T>(odd, ph, o[2 * i + 1]);
-      o[2 * i + 1] = mfma32<T>(odd, pl, o[2 * i + 1]);
+      o[2 * i] = mfma32<T>(even, near, o[2 * i]);
+      o[2 * i + 1] = mfma32<T>(odd, near, o[2 * i + 1]);
+      o[2 * i] = mfma32<T>(even, rest, o[2 * i]);
+      o[2 * i + 1] = mfma32<T>(odd, rest, o[2 * i + 1]);
     }
+    if (more) load_values(next);
+  };
+  int tile = tile0 + wave;
+  if (tile < tile1) {
+    const unsigned first = row_of(tile, look_up(tile));
+    load_keys(first);
+    load_values(first);
+    entry = look_up(tile + W);
+    keep_loads_here();
+    for (; tile + W < tile1; tile += W) work(std::true_type(), tile);
+    work(std::false_type(), tile);
   }
 
   // The block's waves meet.  o[2 i + e] of lane (g, c): head c, dims of the
@@ -224,114 +308,138 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendParams p, int
     s_l[wave][c] = l;
   }
 #pragma unroll
-  for (int i = 0; i < L::pairs; ++i)
+  for (int r = 0; r < 4; ++r) {
+    float* row = s_o[wave][c];
+    const int cc = g * 4 + r;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int d = L::dim(i, g * 4 + r);
-      s_o[wave][c][d] = o[2 * i][r];
-      s_o[wave][c][d + 1] = o[2 * i + 1][r];
-    }
+    for (int i = 0; i < L::n8; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; e += 4)
+        *reinterpret_cast<f32x4*>(row + i * 128 + cc * 8 + e) =
+            f32x4{o[8 * i + e][r], o[8 * i + e + 1][r], o[8 * i + e + 2][r], o[8 * i + e + 3][r]};
+    constexpr int at = 8 * L::n8;
+    if constexpr (L::n4)
+      *reinterpret_cast<f32x4*>(row + L::n8 * 128 + cc * 4) = f32x4{o[at][r], o[at + 1][r], o[at + 2][r], o[at + 3][r]};
+    if constexpr (L::n2)
+      *reinterpret_cast<f32x2*>(row + L::n8 * 128 + L::n4 * 64 + cc * 2) = f32x2{o[at + 4 * L::n4][r], o[at + 4 * L::n4 + 1][r]};
+  }
   __syncthreads();
   const float vs = p.v_scale ? p.v_scale[kh] : 1.f;
-  for (int i = threadIdx.x; i < heads * D; i += 64 * kWaves) {
-    const int h = i / D, d = i % D;
+  for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * W) {
+    const int h = i / (D / 4), d = i % (D / 4) * 4;
     float M = s_m[0][h];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][h]);
-    float acc = 0.f, sum = 0.f;
+    for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][h]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       if (s_l[w][h] == 0.f) continue;         // a wave without tokens
-      const float f = exp2f(s_m[w][h] - M);
-      acc = fmaf(s_o[w][h][d], f, acc);
+      const float f = __builtin_amdgcn_exp2f(s_m[w][h] - M);
+      acc += *reinterpret_cast<const f32x4*>(&s_o[w][h][d]) * f;
       sum = fmaf(s_l[w][h], f, sum);
     }
     const int64_t row = int64_t(b) * p.hq + h0 + h;
     if (runs == 1) {
-      store1<T>(p.out, row * D + d, sum == 0.f ? 0.f : acc / sum * vs);
+      const float k = vs / sum;
+      u32x2 v;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[e] = sum == 0.f ? 0u : pack2<T>(acc[2 * e] * k, acc[2 * e + 1] * k);
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + d) = v;
       if (p.lse && d == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
     } else {
-      part_o[(row * runs + run) * D + d] = acc;
-      if (d == 0) {
-        part_ml[(row * runs + run) * 2] = M;
-        part_ml[(row * runs + run) * 2 + 1] = sum;
-      }
+      *reinterpret_cast<f32x4*>(part_o + (row * runs + run) * D + d) = acc;
+      if (d == 0) *reinterpret_cast<f32x2*>(part_ml + (row * runs + run) * 2) = f32x2{M, sum};
     }
   }
 }
 
-// The runs of one (sequence, query head) joined.  The runs' weights are found
-// once, in LDS; then D / 4 threads read a run's row and the block's other
-// threads read other runs', so a long sequence's rows are in flight together.
-constexpr int kJoinThreads = 512;
-template <class T, int D>
+// The runs of one (sequence, query head) joined, DIMS dims a block.  The runs'
+// weights are found once, in LDS; then DIMS / 4 threads read their part of a
+// run and the block's other threads those of others, four runs under way each.
+template <class T, int DIMS, int kJoinThreads>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams p, int runs, const float* part_o,
                                                                    const float* part_ml) {
-  constexpr int kLanes = D / 4, kRows = kJoinThreads / kLanes;
+  constexpr int kLanes = DIMS / 4, kRows = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave;
   extern __shared__ float s_f[];                // [runs] weights
-  __shared__ float s_red[kJoinThreads / kWave];
+  __shared__ float s_red[2][kWaves];
   __shared__ f32x4 s_acc[kRows][kLanes];
   const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, wave = tid / kWave, r = tid / kLanes, c = tid % kLanes;
   const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * runs;
-  float M = -INFINITY;
-  for (int s = tid; s < runs; s += kJoinThreads) {
+  const f32x4* o = reinterpret_cast<const f32x4*>(part_o + row * runs * p.d + blockIdx.y * DIMS) + c;
+  const int step = p.d / 4;
+  // The first rows and statistics are on their way together.
+  f32x4 early[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) early[x] = o[int64_t(min(r + x * kRows, runs - 1)) * step];
+  const float2 mine = ml[min(tid, runs - 1)];
+  float M = mine.y != 0.f ? mine.x : -INFINITY;
+  for (int s = tid + kJoinThreads; s < runs; s += kJoinThreads) {
     const float2 v = ml[s];
     if (v.y != 0.f) M = fmaxf(M, v.x);
   }
   M = wave_max(M);
-  if (tid % kWave == 0) s_red[tid / kWave] = M;
+  if (tid % kWave == 0) s_red[0][wave] = M;
   __syncthreads();
-  M = s_red[0];
+  M = s_red[0][0];
 #pragma unroll
-  for (int w = 1; w < kJoinThreads / kWave; ++w) M = fmaxf(M, s_red[w]);
-  __syncthreads();
+  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_red[0][w]);
   float sum = 0.f;
   for (int s = tid; s < runs; s += kJoinThreads) {
-    const float2 v = ml[s];
-    const float f = v.y != 0.f ? exp2f(v.x - M) : 0.f;
+    const float2 v = s == tid ? mine : ml[s];
+    const float f = v.y != 0.f ? __builtin_amdgcn_exp2f(v.x - M) : 0.f;
     s_f[s] = f;
     sum = v.y != 0.f ? fmaf(v.y, f, sum) : sum;
   }
   sum = wave_sum(sum);
-  if (tid % kWave == 0) s_red[tid / kWave] = sum;
+  if (tid % kWave == 0) s_red[1][wave] = sum;
   __syncthreads();
   sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < kJoinThreads / kWave; ++w) sum += s_red[w];
+  for (int w = 0; w < kWaves; ++w) sum += s_red[1][w];
 
-  const int r = tid / kLanes, c = tid % kLanes;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (r < kRows) {
-    const f32x4* o = reinterpret_cast<const f32x4*>(part_o + row * runs * D) + c;
-    for (int s = r; s < runs; s += kRows) acc += o[int64_t(s) * kLanes] * s_f[s];
-    s_acc[r][c] = acc;
-  }
-  __syncthreads();
-  if (r != 0) return;
 #pragma unroll
-  for (int i = 1; i < kRows; ++i) acc += s_acc[i][c];
+  for (int x = 0; x < 4; ++x)
+    if (r + x * kRows < runs) acc += early[x] * s_f[r + x * kRows];
+#pragma unroll 4
+  for (int s = r + 4 * kRows; s < runs; s += kRows) acc += o[int64_t(s) * step] * s_f[s];
+  if (r < kRows) s_acc[r][c] = acc;
+  __syncthreads();
+  if (tid >= kLanes) return;
+  acc = s_acc[0][c];
+#pragma unroll 8
+  for (int x = 1; x < kRows; ++x) acc += s_acc[x][c];
   const float k = sum == 0.f ? 0.f : (p.v_scale ? p.v_scale[row % p.hq / (p.hq / p.hk)] : 1.f) / sum;
   u32x2 w;
 #pragma unroll
   for (int i = 0; i < 2; ++i) w[i] = sum == 0.f ? 0u : pack2<T>(acc[2 * i] * k, acc[2 * i + 1] * k);
-  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + c * 4) = w;
-  if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * p.d + blockIdx.y * DIMS + c * 4) = w;
+  if (p.lse && c == 0 && blockIdx.y == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
-// How the tokens of the longest sequence are cut: about four blocks a compute
-// unit over the whole call, and at least two tiles a wave.
+// How the tokens of the longest sequence are cut into runs, by what was
+// measured (us of a call in a graph, bf16, 28 heads of 128 on 4 unless said):
+//   - up to 512 tokens one run: a second launch costs more than it saves (200
+//     tokens 6.5 against 8.6; but 1024 13.3 against 8.8); up to 1024 where
+//     there are 64 blocks without cutting (32 sequences of 1000: 15.7, 20.8);
+//   - one sequence: 512 blocks (131072 tokens 55.6; 57.1 with 1024, 60 with 2048);
+//   - many: up to 4096 blocks, which even out different lengths (24 sequences
+//     of up to 6900, 16 heads of 64 each: 71 against 83 with 1024; equal ones
+//     pay a little, 16 of 65536: 371 against 358);
+//   - and at least a tile for each wave of a block, two where blocks abound.
 struct Plan {
-  int tiles_per_run, runs;
+  int tiles_per_run, runs, waves;
 };
 Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span) {
   const int64_t tiles = (span + kTile - 1) / kTile;
   const int64_t blocks = batch * hk * ((hq / hk + 15) / 16);
-  const int64_t want = std::max<int64_t>(1, (1024 + blocks - 1) / blocks);
-  const int64_t least = 2 * kWaves;
-  int64_t per = std::max(least, (tiles + want - 1) / want);
-  per = (per + kWaves - 1) / kWaves * kWaves;
-  return {int(per), int(std::max<int64_t>(1, (tiles + per - 1) / per))};
+  if (tiles <= (blocks >= 64 ? 32 : 16)) return {int(tiles), 1, tiles > 4 ? 8 : 4};
+  const int64_t want = (std::min<int64_t>(4096, 512 * batch) + blocks - 1) / blocks;
+  int64_t per = std::max<int64_t>(blocks <= 16 ? 4 : 8, (tiles + want - 1) / want);
+  per = (per + 3) / 4 * 4;
+  return {int(per), int((tiles + per - 1) / per), 4};
 }
 
 // Tokens from the first one's tile on that a sequence can span.
@@ -339,18 +447,30 @@ int64_t span_of(int64_t max_length, int64_t window) {
   return window > 0 && window + kTile < max_length ? window + kTile : max_length;
 }
 
-template <class T, bool C8, int D>
-hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  const Plan c = plan(p.batch, p.hq, p.hk, span_of(p.max_length, p.window));
+template <class T, bool C8, int D, int W, bool UNI>
+hipError_t launch_form(const AttendParams& p, const Plan& c, hipStream_t stream) {
   const int64_t rows = int64_t(p.batch) * p.hq;
   float* part_ml = static_cast<float*>(p.workspace);
   float* part_o = part_ml + (rows * c.runs * 2 + 63) / 64 * 64;
   const dim3 grid(unsigned(c.runs), unsigned(p.hk * ((p.hq / p.hk + 15) / 16)), unsigned(p.batch));
-  attend_kernel<T, C8, D><<<grid, dim3(64 * kWaves), 0, stream>>>(p, c.tiles_per_run, c.runs, part_o, part_ml);
+  attend_kernel<T, C8, D, W, UNI><<<grid, dim3(64 * W), 0, stream>>>(p, c.tiles_per_run, c.runs, part_o, part_ml);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || c.runs == 1) return e;
-  attend_join_kernel<T, D><<<dim3(unsigned(rows)), dim3(kJoinThreads), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml);
+  // Few rows: more blocks, each of a part of the dims (28 rows, 256 runs of 128
+  // dims 5.1 -> 2.9 us); many rows need no more blocks (896 rows, 4 runs: 5 us more).
+  if (rows < 256)
+    attend_join_kernel<T, 32, 512><<<dim3(unsigned(rows), D / 32), dim3(512), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml);
+  else
+    attend_join_kernel<T, D, 256><<<dim3(unsigned(rows), 1), dim3(256), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml);
   return hipGetLastError();
+}
+
+template <class T, bool C8, int D>
+hipError_t launch(const AttendParams& p, hipStream_t stream) {
+  const Plan c = plan(p.batch, p.hq, p.hk, span_of(p.max_length, p.window));
+  if (p.page % kTile == 0)
+    return c.waves == 8 ? launch_form<T, C8, D, 8, true>(p, c, stream) : launch_form<T, C8, D, 4, true>(p, c, stream);
+  return c.waves == 8 ? launch_form<T, C8, D, 8, false>(p, c, stream) : launch_form<T, C8, D, 4, false>(p, c, stream);
 }
 
 template <class T, bool C8>

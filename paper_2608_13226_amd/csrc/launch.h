@@ -265,6 +265,8 @@ struct AttendParams {
   int64_t pages;                  // pages * hk * page < 2^32
   int64_t max_length;             // 1 <= max_length <= width * page < 2^31
   int batch, hq, hk, d, page, width;
+  unsigned page_magic, page_shift;  // t / page = (2 t * magic >> 32) >> shift for 0 <= t < 2^31:
+                                  // shift = ceil(log2 page), magic = ceil(2^(31 + shift) / page)
   int window;                     // 0: none
   float scale;
   bool cache8;
