@@ -165,6 +165,7 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   const int run = blockIdx.x, kh = blockIdx.y / head_tiles, h0 = kh * group + blockIdx.y % head_tiles * 16;
   const int heads = min(16, (kh + 1) * group - h0);
   const int b = blockIdx.z;
+  if (run >= runs) return;
 
   const int hi = max(0, int(min(int64_t(__builtin_amdgcn_readfirstlane(p.lengths[b])), p.max_length)));
   const int lo = p.window > 0 ? max(0, hi - p.window) : 0;
@@ -425,9 +426,9 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams 
 //     tokens 6.5 against 8.6; but 1024 13.3 against 8.8); up to 1024 where
 //     there are 64 blocks without cutting (32 sequences of 1000: 15.7, 20.8);
 //   - one sequence: 512 blocks (131072 tokens 55.6; 57.1 with 1024, 60 with 2048);
-//   - many: up to 4096 blocks, which even out different lengths (24 sequences
-//     of up to 6900, 16 heads of 64 each: 71 against 83 with 1024; equal ones
-//     pay a little, 16 of 65536: 371 against 358);
+//   - many: up to 2048 blocks, which even out different lengths (24 sequences
+//     of up to 6900, 16 heads of 64 each: 73 against 82 with 1024 and 88 with
+//     512; equal ones do not care, 16 of 65536: 369, 379 with 4096);
 //   - and at least a tile for each wave of a block, two where blocks abound.
 struct Plan {
   int tiles_per_run, runs, waves;
@@ -436,7 +437,7 @@ Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span) {
   const int64_t tiles = (span + kTile - 1) / kTile;
   const int64_t blocks = batch * hk * ((hq / hk + 15) / 16);
   if (tiles <= (blocks >= 64 ? 32 : 16)) return {int(tiles), 1, tiles > 4 ? 8 : 4};
-  const int64_t want = (std::min<int64_t>(4096, 512 * batch) + blocks - 1) / blocks;
+  const int64_t want = (std::min<int64_t>(2048, 512 * batch) + blocks - 1) / blocks;
   int64_t per = std::max<int64_t>(blocks <= 16 ? 4 : 8, (tiles + want - 1) / want);
   per = (per + 3) / 4 * 4;
   return {int(per), int((tiles + per - 1) / per), 4};
@@ -452,7 +453,12 @@ hipError_t launch_form(const AttendParams& p, const Plan& c, hipStream_t stream)
   const int64_t rows = int64_t(p.batch) * p.hq;
   float* part_ml = static_cast<float*>(p.workspace);
   float* part_o = part_ml + (rows * c.runs * 2 + 63) / 64 * 64;
-  const dim3 grid(unsigned(c.runs), unsigned(p.hk * ((p.hq / p.hk + 15) / 16)), unsigned(p.batch));
+  // Blocks go to the eight XCDs in turn: with an odd count of them a sequence, the
+  // runs that short sequences lack are missing from all alike (16 sequences of
+  // 1 to 65536 tokens in 32 runs 246 us, with a block more 221).  One sequence
+  // lacks none, and its blocks are as many as fill the chip evenly (131072
+  // tokens e4m3 31 us, with a block more 36).
+  const dim3 grid(unsigned(p.batch > 1 ? c.runs | 1 : c.runs), unsigned(p.hk * ((p.hq / p.hk + 15) / 16)), unsigned(p.batch));
   attend_kernel<T, C8, D, W, UNI><<<grid, dim3(64 * W), 0, stream>>>(p, c.tiles_per_run, c.runs, part_o, part_ml);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || c.runs == 1) return e;
