@@ -62,6 +62,12 @@ __device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float 
   w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(c), e4m3_clamp(d), w, true);
   return uint32_t(w);
 }
+// The same for floats that round to at most +-448 as they are.
+__device__ __forceinline__ uint32_t pack4_e4m3_inside(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  return uint32_t(w);
+}
 
 // Element i of an array of T as float, and back (rounded to nearest even).
 template <class T>

@@ -98,3 +98,21 @@ def test_large_values_do_not_overflow_the_output_scale():
     x[2] *= 1e-30
     got = cp.rms_norm(x, w, eps=0.0, quantize=True)
     _check(x, w, None, 0.0, got, True)
+
+
+@pytest.mark.parametrize("xs,ws", [(1e-20, 1e-15), (1e17, 1e18), (1e-4, 1e-30), (1e10, 1e-25), (3e18, 1.0)])
+def test_products_near_the_ends_of_float32(xs, ws):
+    """Rows and weights whose products leave the range that the codes' one factor covers."""
+    import paper_2608_13226_amd as cp
+    x, w, _ = _data(5, 1024, F32, False)
+    x, w = x * xs, w * ws
+    x[3] = 0
+    got = cp.rms_norm(x, w, eps=0.0 if xs < 1e10 else 1e-6, quantize=True)
+    y, _ = ref.rms_norm(x, w, 0.0 if xs < 1e10 else 1e-6, None)
+    y = torch.nan_to_num(y) if xs < 1e10 else y
+    keep = [0, 1, 2, 4]
+    # 0 / 0 in the formula: the zero row with eps = 0.
+    assert xs >= 1e10 or bool(torch.isnan(got.scale[3]))
+    scale = y.abs().amax(1) / 448.0
+    ref.assert_close(got.scale[keep], scale[keep], F32, 2.0 ** -24 * 96 * scale[keep], "scale")
+    ref.assert_e4m3(got.out.view(torch.uint8)[keep].view(got.out.dtype), (y / got.scale.cpu().double()[:, None])[keep], "codes")
