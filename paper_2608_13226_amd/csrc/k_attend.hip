@@ -292,10 +292,11 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   int tile = tile0 + wave;
   if (tile < tile1) {
     const unsigned first = row_of(tile, look_up(tile));
+    // In the order of the loop, so that its waits are for just what they need.
     load_keys(first);
-    load_values(first);
     entry = look_up(tile + W);
     keep_loads_here();
+    load_values(first);
     for (; tile + W < tile1; tile += W) work(std::true_type(), tile);
     work(std::false_type(), tile);
   }

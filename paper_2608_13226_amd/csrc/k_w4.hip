@@ -285,6 +285,13 @@ __device__ __forceinline__ float add2<F16>(uint32_t w, float c) {
 // the block brings 256 k of it to LDS at a time, as operands, with the groups'
 // sums beside them, while it works on the 256 before.  Waves: 8 by outputs (16
 // each) times 2 by k; codes are loaded two turns ahead.
+//
+// Bound by instruction issue: at 64 x 3584 x 28672, groups of 64, 32 us (1.9
+// TB/s of codes, 410 TFLOP/s); of a SIMD's cycles 54 % issue vector
+// instructions (141 a wave and turn, 28 of them to widen the codes) and the
+// matrix cores work in 31 %.  32 outputs a wave read LDS half as often but do not
+// fit the registers of 16 waves (44 us; 40 with 8 waves), turns of 512 k change
+// nothing (34).
 constexpr int kWideRows = 128;
 constexpr int kWideGroups = 64;                   // whose scales are in LDS at a time
 template <class T, bool X8, int SPAN, int MT>
@@ -344,18 +351,19 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
   // One turn: its x is in s_x[buf], its codes in w[buf]; the turn after's x is
   // in xv[1 - buf] or on its way.
   auto turn_of = [&](auto more, int buf, int turn) {
-    float scale[kGroups], zero = 0.f;             // lane group g gives the zero points of the run's group g
     uint32_t v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = w[buf][j];
     if constexpr (SPAN < 4) transpose4(v);
+    auto place = [&](int h) {
+      return (wave % 8 * 16 + c) * kPitch + min(group_of(p, turn * 8 + half * 4 + h * SPAN), last_group) - g0;
+    };
+    float scale[kGroups];
 #pragma unroll
-    for (int h = 0; h < kGroups; ++h) {
-      const int at = (wave % 8 * 16 + c) * kPitch + min(group_of(p, turn * 8 + half * 4 + h * SPAN), last_group) - g0;
-      const float s = widen1<T>(s_scale[at]);
-      scale[h] = 512.f * s;
-      zero = g == h ? -s * float(s_zero[at]) : zero;
-    }
+    for (int h = 0; h < kGroups; ++h) scale[h] = 512.f * widen1<T>(s_scale[place(h)]);
+    // Lane group g gives the zero points of the run's group g.
+    const int own = place(min(g, kGroups - 1));
+    const float zero = g < kGroups ? -widen1<T>(s_scale[own]) * float(s_zero[own]) : 0.f;
     __builtin_amdgcn_sched_barrier(0);
     if (more || turn + 2 < turns) {
       // x first: what waits for it, at the end of the next turn, then does not
@@ -367,12 +375,11 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
     for (int h = 0; h < kGroups; ++h) {
       f32x4 acc[MT];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
       for (int j = h * SPAN; j < (h + 1) * SPAN; ++j) {
         const u32x4 a = codes<T>(v[j]);
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = mfma32<T>(s_x[buf][half][j][t][g * 16 + (c ^ (j * 4 + g))], a, acc[t]);
+        for (int t = 0; t < MT; ++t)
+          acc[t] = mfma32<T>(s_x[buf][half][j][t][g * 16 + (c ^ (j * 4 + g))], a, j == h * SPAN ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[t]);
       }
 #pragma unroll
       for (int t = 0; t < MT; ++t)
@@ -390,23 +397,29 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
   load_w(&w[1], 1);
   keep_x(std::false_type(), xv[0], 0, 0);
   lds_barrier();
-  // kWideGroups groups are `block` turns, an even number (group / 4).  While two
-  // more turns are certain nothing about the loads is conditional, so that
-  // each wait is for just what it needs.
+  // kWideGroups groups are `block` turns, an even number (group / 4).
   const int block = kWideGroups * p.group / 256;
-  for (int turn = 0; turn < turns;) {
-    const int stop = min(turn + block, turns);
+  int turn = 0, stop = 0;
+  auto next_scales = [&] {
+    stop = turn + block;
     g0 = group_of(p, turn * 8);
     keep_scales<kPitch>(p, first, kWideRows, g0, min(kWideGroups, last_group + 1 - g0), s_scale, s_zero);
     lds_barrier();
-    for (; turn + 4 <= turns && turn < stop; turn += 2) {
+  };
+  // While two more turns are certain nothing about the loads is conditional, so
+  // that each wait is for just what it needs.
+  while (turn + 4 <= turns) {
+    next_scales();
+    const int end = min(stop, (turns - 2) / 2 * 2);
+    for (; turn < end; turn += 2) {
       turn_of(std::true_type(), 0, turn);
       turn_of(std::true_type(), 1, turn + 1);
     }
-    for (; turn < stop; turn += 2) {
-      turn_of(std::false_type(), 0, turn);
-      if (turn + 1 < turns) turn_of(std::false_type(), 1, turn + 1);
-    }
+  }
+  for (; turn < turns; turn += 2) {
+    if (turn == stop) next_scales();
+    turn_of(std::false_type(), 0, turn);
+    if (turn + 1 < turns) turn_of(std::false_type(), 1, turn + 1);
   }
 
   // The halves meet.  y[t][r] of lane (g, c): output c of row 16 t + 4 g + r.
