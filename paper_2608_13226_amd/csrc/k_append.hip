@@ -10,6 +10,8 @@
 // position and 24 of frequency do not fit a float32 product, whose error
 // would reach whole hundredths of a radian at positions of 10^5), the sine
 // and cosine of the fraction are float32.
+#include <algorithm>
+
 #include "launch.h"
 #include "serve.h"
 
@@ -21,6 +23,7 @@ namespace {
 template <class T, int VEC>
 __device__ __forceinline__ void load_run(const void* p, int64_t i, float* x) {
   if constexpr (VEC == 8) load8<T>(p, i, x);
+  else if constexpr (VEC == 4) load4<T>(p, i, x);
   else x[0] = load1<T>(p, i);
 }
 template <class C, int VEC>
@@ -30,12 +33,13 @@ __device__ __forceinline__ void store_run(void* p, int64_t i, float* x, float de
     for (int j = 0; j < VEC; ++j) x[j] /= den;
   }
   if constexpr (VEC == 8) store8<C>(p, i, x);
+  else if constexpr (VEC == 4) store4<C>(p, i, x);
   else store1<C>(p, i, x[0]);
 }
 
 // T: type of the projections, C: of the caches.  VEC = 8 needs 16-byte aligned
 // rows, d % 8 == 0 and pairs that come in whole runs (rot % 16 == 0, or 8
-// when interleaved); VEC = 1 is for everything else.
+// when interleaved); VEC = 4 half of each; VEC = 1 is for everything else.
 template <class T, class C, int VEC, bool INTER>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p) {
   extern __shared__ float s_turn[];           // [rot / 2] cosines, [rot / 2] sines
@@ -64,7 +68,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p) {
   const int runs = pair_runs + (p.d - p.rot) / VEC;
   const int hq = p.q ? p.hq : 0;
   const int total = (hq + p.hk) * runs;
-  for (int w = threadIdx.x; w < total; w += blockDim.x) {
+  const int first = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
+  for (int w = first; w < total; w += step) {
     const int head = w / runs, r = w - head * runs;
     const bool is_q = head < hq;
     const int kh = head - hq;
@@ -112,7 +117,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p) {
   }
   if (!keep) return;
   const int vruns = p.d / VEC;
-  for (int w = threadIdx.x; w < p.hk * vruns; w += blockDim.x) {
+  // The values follow the rest, for the threads that have less of it.
+  for (int w = (first - total % step + step) % step; w < p.hk * vruns; w += step) {
     const int kh = w / vruns, e = (w - kh * vruns) * VEC;
     float x[VEC];
     load_run<T, VEC>(p.v, t * p.v_stride + int64_t(kh) * p.d + e, x);
@@ -122,18 +128,33 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p) {
 
 template <class T, class C, int VEC, bool INTER>
 hipError_t launch(const KvAppendParams& p, hipStream_t stream) {
-  kv_append_kernel<T, C, VEC, INTER><<<dim3(unsigned(p.tokens)), dim3(256), size_t(p.rot) * sizeof(float), stream>>>(p);
+  // Few tokens: their heads are spread over more blocks, up to 2048, which find
+  // the angles again, so that fewer threads have a second run to wait for (one
+  // token of 64 + 16 heads of 128 4.9 -> 2.9 us, 300 tokens of them 5.9 -> 4.9;
+  // with 4096 blocks 1638 tokens of 28 + 4 heads take 9.0 instead of 8.0).
+  const int64_t work = (int64_t(p.q ? p.hq : 0) + 2 * p.hk) * (p.d / VEC);
+  const unsigned y = unsigned(std::max<int64_t>(1, std::min<int64_t>(2048 / p.tokens, (work + 255) / 256)));
+  kv_append_kernel<T, C, VEC, INTER><<<dim3(unsigned(p.tokens), y), dim3(256), size_t(p.rot) * sizeof(float), stream>>>(p);
   return hipGetLastError();
 }
 
-bool aligned(const void* q, int64_t stride) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0 && stride % 8 == 0; }
+bool aligned(const void* q, int64_t stride, int bytes) {
+  return reinterpret_cast<uintptr_t>(q) % bytes == 0 && stride * 2 % bytes == 0;
+}
+
+template <class T, class C, bool INTER>
+hipError_t launch_width(const KvAppendParams& p, hipStream_t stream) {
+  auto fits = [&](int vec) {
+    return p.d % vec == 0 && p.rot % (INTER ? vec : 2 * vec) == 0 && (!p.q || aligned(p.q, p.q_stride, 2 * vec)) &&
+           aligned(p.k, p.k_stride, 2 * vec) && aligned(p.v, p.v_stride, 2 * vec);
+  };
+  if (fits(8)) return launch<T, C, 8, INTER>(p, stream);
+  return fits(4) ? launch<T, C, 4, INTER>(p, stream) : launch<T, C, 1, INTER>(p, stream);
+}
 
 template <class T, class C>
 hipError_t launch_type(const KvAppendParams& p, hipStream_t stream) {
-  const bool wide = p.d % 8 == 0 && p.rot % (p.interleaved ? 8 : 16) == 0 && (!p.q || aligned(p.q, p.q_stride)) &&
-                    aligned(p.k, p.k_stride) && aligned(p.v, p.v_stride);
-  if (p.interleaved) return wide ? launch<T, C, 8, true>(p, stream) : launch<T, C, 1, true>(p, stream);
-  return wide ? launch<T, C, 8, false>(p, stream) : launch<T, C, 1, false>(p, stream);
+  return p.interleaved ? launch_width<T, C, true>(p, stream) : launch_width<T, C, false>(p, stream);
 }
 
 }  // namespace

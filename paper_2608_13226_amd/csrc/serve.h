@@ -146,6 +146,26 @@ __device__ __forceinline__ void store8<E4m3>(void* p, int64_t i, const float* x)
   *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p) + i) = w;
 }
 
+// The same with four (8-byte aligned; 4-byte for e4m3), of 16-bit types.
+template <class T>
+__device__ __forceinline__ void load4(const void* p, int64_t i, float* x) {
+  const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float2 f = unpack2<T>(w[j]);
+    x[2 * j] = f.x;
+    x[2 * j + 1] = f.y;
+  }
+}
+template <class T>
+__device__ __forceinline__ void store4(void* p, int64_t i, const float* x) {
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + i) = u32x2{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+}
+template <>
+__device__ __forceinline__ void store4<E4m3>(void* p, int64_t i, const float* x) {
+  *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = pack4_e4m3(x[0], x[1], x[2], x[3]);
+}
+
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);

@@ -71,7 +71,10 @@ def _run(tokens, hq, hk, d, rot, page, t, c, interleaved, pad=0, magnitude=1.0, 
 @pytest.mark.parametrize("tokens,hq,hk,d,rot,page,t", [
     (1, 28, 4, 128, 128, 16, BF), (3, 4, 4, 64, 32, 1, F16), (37, 8, 1, 256, 256, 7, BF), (5, 6, 2, 96, 96, 50, F16),
     (130, 16, 2, 128, 64, 64, BF), (9, 3, 3, 80, 20, 16, BF), (2, 2, 1, 10, 6, 3, F16), (4, 1, 1, 7, 2, 5, BF),
-    (11, 4, 2, 192, 0, 16, BF), (6, 5, 5, 72, 72, 32, BF)])
+    (11, 4, 2, 192, 0, 16, BF), (6, 5, 5, 72, 72, 32, BF),
+    # runs of four; many heads of few tokens, spread over blocks
+    (21, 8, 2, 96, 24, 16, F16), (7, 3, 1, 36, 8, 4, BF), (1, 112, 16, 96, 48, 100, BF), (600, 3, 1, 64, 64, 16, F16),
+    (1025, 2, 1, 128, 128, 64, BF)])
 def test_append(tokens, hq, hk, d, rot, page, t, interleaved, c8):
     print(f"append tokens={tokens} heads={hq}/{hk} d={d} rot={rot} page={page} {t} inter={interleaved} c8={c8}", flush=True)
     _run(tokens, hq, hk, d, rot, page, t, E4M3 if c8 else t, interleaved)
