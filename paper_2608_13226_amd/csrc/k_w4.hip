@@ -108,25 +108,29 @@ __device__ __forceinline__ int group_of(const W4Params& p, int r) {
   return int(unsigned((uint64_t(r) * p.group_magic) >> 32) + unsigned(r) * p.group_one);
 }
 
-// The scales and zero points of a lane's output at a run of 128 k.
-template <class T, int SPAN>
+// The scales and zero points of a lane's output.  A lane's load of two bytes
+// and one touches as many cache lines as one of its codes, so lane group g
+// loads those of the g-th of the next four groups that the wave meets (of SPAN
+// runs), and they trade.
 struct Scales {
-  static constexpr int kGroups = 4 / SPAN;
-  uint16_t s[kGroups];
-  uint8_t z[kGroups];
+  uint16_t s;
+  uint8_t z;
 
   // lane: the output's first group, from the block's first output's on.
-  __device__ __forceinline__ void load(const W4Params& p, int64_t n0, unsigned lane, int groups, int kb) {
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j) {
-      const int64_t base = n0 * groups + min(group_of(p, kb / 32 + j * SPAN), groups - 1);
-      s[j] = (static_cast<const uint16_t*>(p.scale) + base)[lane];
-      // Without zero points a byte of the scales is read in their place and dropped.
-      z[j] = ((p.zero ? p.zero : static_cast<const uint8_t*>(p.scale)) + base)[lane];
-    }
+  __device__ __forceinline__ void load(const W4Params& p, int64_t n0, unsigned lane, int groups, int run) {
+    const int64_t base = n0 * groups;
+    const unsigned at = lane + unsigned(min(group_of(p, run), groups - 1));
+    s = (static_cast<const uint16_t*>(p.scale) + base)[at];
+    // Without zero points a byte of the scales is read in their place and dropped.
+    z = ((p.zero ? p.zero : static_cast<const uint8_t*>(p.scale)) + base)[at];
   }
-  __device__ __forceinline__ float scale(int j) const { return unpack2<T>(s[j]).x; }
-  __device__ __forceinline__ float zero(const W4Params& p, int j) const { return p.zero ? float(z[j]) : 8.f; }
+  // What lane group d loaded -> all[d], of every lane.
+  __device__ __forceinline__ void trade(const W4Params& p, uint32_t* all) const {
+    const uint32_t v = s | uint32_t(p.zero ? z : 8) << 16;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) all[d] = v;
+    transpose4(all);
+  }
 };
 
 // The 32 codes of lane group g at a run of 128 k; lane: the output's first byte.
@@ -169,21 +173,26 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
   auto k_of = [&](int kb, int j) { return kb + (SPAN < 4 ? j * 32 + g * 8 : g * 32 + j * 8); };
   struct Stage {
     u32x4 w[RT];
-    Scales<T, SPAN> sc[RT];
     RawX<X8> x[4];
   } stage;
+  Scales scales[RT];
+  const int step = waves * 128;
   // What a run needs, on its way while the run before is worked on.
   auto load = [&](Stage& s, int kb) {
 #pragma unroll
     for (int i = 0; i < RT; ++i) s.w[i] = load_codes(p, n0, row[i] * unsigned(p.k / 2), kb, g);
 #pragma unroll
     for (int j = 0; j < 4; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_of(kb, j), p.k - 8)));
-#pragma unroll
-    for (int i = 0; i < RT; ++i) s.sc[i].load(p, n0, row[i] * unsigned(groups), groups, kb);
     keep_loads_here();
   };
-  const int step = waves * 128;
-  auto use = [&](auto more, Stage& s, int kb) {
+  auto load_scales = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+      scales[i].load(p, n0, row[i] * unsigned(groups), groups, (kb + g / kGroups * step) / 32 + g % kGroups * SPAN);
+    keep_loads_here();
+  };
+  // Run t of SPAN at kb; all: their scales and zero points.
+  auto use = [&](Stage& s, int kb, int t, uint32_t (*all)[4], bool more, bool more_scales) {
     u32x4 a[RT][4], b[4];
     float sc[RT][kGroups], z[RT][kGroups];
 #pragma unroll
@@ -193,12 +202,15 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
       operands<T, SPAN>(s.w[i], a[i]);
 #pragma unroll
       for (int h = 0; h < kGroups; ++h) {
-        sc[i][h] = 512.f * s.sc[i].scale(h);
-        z[i][h] = -s.sc[i].scale(h) * s.sc[i].zero(p, h);
+        const uint32_t v = all[i][t * kGroups + h];
+        const float scale = unpack2<T>(v).x;
+        sc[i][h] = 512.f * scale;
+        z[i][h] = -scale * float(v >> 16);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (more || kb + step < p.k) load(s, kb + step);
+    if (more_scales) load_scales(kb + SPAN * step);
+    if (more) load(s, kb + step);
 #pragma unroll
     for (int h = 0; h < kGroups; ++h) {
       f32x4 sum = {0.f, 0.f, 0.f, 0.f}, acc[RT];
@@ -217,9 +229,18 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
     }
   };
   int kb = wave * 128;
+  load_scales(kb);
   load(stage, kb);
-  for (; kb + step < p.k; kb += step) use(std::true_type(), stage, kb);
-  if (kb < p.k) use(std::false_type(), stage, kb);
+  while (kb < p.k) {
+    uint32_t all[RT][4];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) scales[i].trade(p, all[i]);
+#pragma unroll
+    for (int t = 0; t < SPAN; ++t, kb += step) {
+      if (kb >= p.k) break;
+      use(stage, kb, t, all, kb + step < p.k, t == 0 && kb + SPAN * step < p.k);
+    }
+  }
 
   // y[i][r] of lane (g, c): output 16 i + c of row 4 g + r.
 #pragma unroll
