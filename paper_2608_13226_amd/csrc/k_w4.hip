@@ -148,11 +148,38 @@ __device__ __forceinline__ void operands(u32x4 w, u32x4* a) {
   for (int j = 0; j < 4; ++j) a[j] = codes<T>(v[j]);
 }
 
+// Neighbouring lanes' x -> x[0 .. SHARE - 1] of them all.
+template <int SHARE>
+__device__ __forceinline__ void spread(u32x4 v, u32x4* x) {
+  auto moved = [](uint32_t w, auto ctrl) { return uint32_t(__builtin_amdgcn_mov_dpp(int(w), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  if constexpr (SHARE == 1) x[0] = v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (SHARE == 2) {
+      x[0][e] = moved(v[e], std::integral_constant<int, 0xa0>());   // quad: 0 0 2 2
+      x[1][e] = moved(v[e], std::integral_constant<int, 0xf5>());   // quad: 1 1 3 3
+    }
+    if constexpr (SHARE == 4) {
+      x[0][e] = moved(v[e], std::integral_constant<int, 0x00>());   // quad: 0 0 0 0
+      x[1][e] = moved(v[e], std::integral_constant<int, 0x55>());   // quad: 1 1 1 1
+      x[2][e] = moved(v[e], std::integral_constant<int, 0xaa>());   // quad: 2 2 2 2
+      x[3][e] = moved(v[e], std::integral_constant<int, 0xff>());   // quad: 3 3 3 3
+    }
+  }
+}
+
 // Up to 16 rows.  A wave works on 16 RT outputs, whose x it reads from the
 // caches and puts in order once for all of them, at every waves-th run of 128
 // k; the sums of the block's waves meet in LDS.
-template <class T, bool X8, int SPAN, int RT>
-__global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
+//
+// What a compute unit can fill bounds it, and at 64 bytes a cycle a run's x,
+// 16 rows of it, takes 64 cycles beside some 95 of 16 outputs' codes.  Up to 16
+// / SHARE rows, SHARE neighbouring lanes hold one row: each loads its share of
+// the row's x once and they pass it on; row r of x is then the product's rows
+// SHARE r to SHARE r + SHARE - 1, all alike.  At 1 x 3584 x 28672, groups of
+// 128, 11.8 us (4.5 TB/s), at 16 rows 17.8 (3.0 TB/s).
+template <class T, bool X8, int SPAN, int RT, int SHARE>
+__global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p) {
   constexpr int kGroups = 4 / SPAN;
   extern __shared__ float s_part[];               // [waves][RT][16][17]
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -164,7 +191,7 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
   unsigned row[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) row[i] = unsigned(min(int64_t(i * 16 + c), p.n - 1 - n0));
-  const unsigned xrow = unsigned(min(int64_t(c), p.m - 1 - m0)) * unsigned(p.k);
+  const unsigned xrow = unsigned(min(int64_t(c / SHARE), p.m - 1 - m0)) * unsigned(p.k);
   const uint8_t* xbase = static_cast<const uint8_t*>(p.x) + m0 * p.k * (X8 ? 1 : 2);
   f32x4 y[RT];
 #pragma unroll
@@ -173,7 +200,7 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
   auto k_of = [&](int kb, int j) { return kb + (SPAN < 4 ? j * 32 + g * 8 : g * 32 + j * 8); };
   struct Stage {
     u32x4 w[RT];
-    RawX<X8> x[4];
+    RawX<X8> x[4 / SHARE];
   } stage;
   Scales scales[RT];
   const int step = waves * 128;
@@ -182,7 +209,7 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
 #pragma unroll
     for (int i = 0; i < RT; ++i) s.w[i] = load_codes(p, n0, row[i] * unsigned(p.k / 2), kb, g);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_of(kb, j), p.k - 8)));
+    for (int j = 0; j < 4 / SHARE; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_of(kb, j * SHARE + c % SHARE), p.k - 8)));
     keep_loads_here();
   };
   auto load_scales = [&](int kb) {
@@ -196,7 +223,8 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
     u32x4 a[RT][4], b[4];
     float sc[RT][kGroups], z[RT][kGroups];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = s.x[j].template operand<T>(SPAN == 4 || k_of(kb, j) < p.k);
+    for (int j = 0; j < 4 / SHARE; ++j)
+      spread<SHARE>(s.x[j].template operand<T>(SPAN == 4 || k_of(kb, j * SHARE + c % SHARE) < p.k), b + j * SHARE);
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       operands<T, SPAN>(s.w[i], a[i]);
@@ -225,7 +253,7 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[i][r] = fmaf(sc[i][h], acc[i][r], fmaf(z[i][h], sum[r], y[i][r]));
+        for (int r = 0; r < 4; r += SHARE) y[i][r] = fmaf(sc[i][h], acc[i][r], fmaf(z[i][h], sum[r], y[i][r]));
     }
   };
   int kb = wave * 128;
@@ -246,11 +274,11 @@ __global__ __launch_bounds__(512, 2) void w4_few_kernel(W4Params p) {
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s_part[((wave * RT + i) * 16 + g * 4 + r) * 17 + c] = y[i][r];
+    for (int r = 0; r < 4; r += SHARE) s_part[((wave * RT + i) * 16 + g * 4 + r) * 17 + c] = y[i][r];
   __syncthreads();
-  for (int e = threadIdx.x; e < RT * 256; e += blockDim.x) {
-    const int i = e / 16 % RT, mr = e / (16 * RT);
-    const int64_t m = m0 + mr, n = n0 + i * 16 + e % 16;
+  for (int e = threadIdx.x; e < RT * 256 / SHARE; e += blockDim.x) {
+    const int i = e / 16 % RT, mr = e / (16 * RT) * SHARE;
+    const int64_t m = m0 + mr / SHARE, n = n0 + i * 16 + e % 16;
     if (m >= p.m || n >= p.n) continue;
     float v = 0.f;
     for (int x = 0; x < waves; ++x) v += s_part[((x * RT + i) * 16 + mr) * 17 + e % 16];
@@ -473,30 +501,43 @@ hipError_t launch_wide(const W4Params& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <class T, bool X8, int SPAN, int RT>
+template <class T, bool X8, int SPAN, int RT, int SHARE>
 hipError_t launch_few(const W4Params& p, hipStream_t stream) {
-  const int waves = std::min(RT == 4 ? 4 : 8, (p.k + 127) / 128);
+  const int most = RT == 4 ? 4 : SHARE == 4 && p.k >= 8192 ? 16 : 8, waves = std::min(most, (p.k + 127) / 128);
   const dim3 grid(unsigned((p.n + 16 * RT - 1) / (16 * RT)), unsigned((p.m + 15) / 16));
-  w4_few_kernel<T, X8, SPAN, RT><<<grid, dim3(kWave * waves), size_t(waves) * RT * 272 * sizeof(float), stream>>>(p);
+  w4_few_kernel<T, X8, SPAN, RT, SHARE><<<grid, dim3(kWave * waves), size_t(waves) * RT * 272 * sizeof(float), stream>>>(p);
   return hipGetLastError();
 }
 
-// Which kernel (times of one call in a graph, k = 3584, groups of 128, us):
+// Which kernel (m rows; times of one call in a graph, k = 3584 and groups of
+// 128 where not said, us; a tile is 16 rows by 16 outputs):
 //   - more than 16 rows and many outputs: the wide one, whose time hardly
 //     depends on n up to a block a compute unit (64 rows: 29 at n = 4608, 30 at
-//     28672; 32 rows: 22 at 28672), while that of the other grows with it (64
-//     rows: 19 and 58; 32 rows: 12 and 35);
-//   - otherwise 16 outputs a wave while there are fewer than two waves' worth a
-//     compute unit (one row, n = 1500: 3.8 against 5.3 with 32; n = 4608: 6.4
-//     against 5.7), 64 when there are plenty (16 rows, n = 28672: 27 against
-//     30; one row 14.8 against 15.8; but one row, n = 4608 10.1).
+//     28672; 32 rows: 21 at 28672), while that of the other grows with it (64
+//     rows: 17 and 58; 32 rows: 10 and 31);
+//   - up to 4 rows, lanes share x four ways: 11.9 against 13.3 at n = 28672, 9.5
+//     against 10.7 at n = 3584, k = 14336; up to 8 rows, two ways: 12.8 against
+//     14.9, 10.4 against 15.3.  Shared four ways, more outputs a wave gain
+//     nothing (n = 4608: 4.8 and 4.7; 28672: 12.1 and 12.2);
+//   - 16 outputs a wave while there are fewer tiles than compute units (16 rows,
+//     n = 3584, k = 14336: 19 against 24 with 32); then 32 (n = 4608: 7.4
+//     against 10.2 with 16 and 10.3 with 64); and 64 when 32 would
+//     make more than a block a compute unit (32 rows, n = 4608: 10.6
+//     against 12.3; n = 28672, 16 rows: 17.8 against 22.1), or, where k is short
+//     and a block's start weighs, more than three (64 rows, n = 8000, k = 1024: 8.4
+//     against 10.2; but 48 rows 8.4 against 7.9);
+//   - 8 waves a block, 16 for a long k (one row, n = 3584, k = 14336: 8.4 against
+//     9.5; but n = 28672, k = 3584 14.1 against 12.1), 4 where each holds 64
+//     outputs.
 template <class T, bool X8, int SPAN>
 hipError_t launch_span(const W4Params& p, hipStream_t stream) {
   if (p.m > 16 && p.n >= (p.m > 32 ? 8192 : 10240))
     return p.m <= 32 ? launch_wide<T, X8, SPAN, 2>(p, stream) : launch_wide<T, X8, SPAN, 4>(p, stream);
   const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
-  if (tiles >= 1024) return launch_few<T, X8, SPAN, 4>(p, stream);
-  return tiles >= 256 ? launch_few<T, X8, SPAN, 2>(p, stream) : launch_few<T, X8, SPAN, 1>(p, stream);
+  if (p.m <= 4) return launch_few<T, X8, SPAN, 1, 4>(p, stream);
+  if (p.m <= 8) return tiles < 256 ? launch_few<T, X8, SPAN, 1, 2>(p, stream) : launch_few<T, X8, SPAN, 2, 2>(p, stream);
+  if (tiles < 256) return launch_few<T, X8, SPAN, 1, 1>(p, stream);
+  return tiles <= (p.k < 2048 ? 1536 : 512) ? launch_few<T, X8, SPAN, 2, 1>(p, stream) : launch_few<T, X8, SPAN, 4, 1>(p, stream);
 }
 
 template <class T, bool X8>

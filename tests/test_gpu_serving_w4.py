@@ -100,3 +100,27 @@ def test_fed_by_the_norm():
     r = cp.rms_norm(x, gain, quantize=True)
     _, w, s, z, _ = _data(6, 200, 1024, 128, BF, False, True)
     _check(r.out, w, s, z, r.scale, out_dtype=F32)
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 6, 8, 9])
+@pytest.mark.parametrize("n,k,group", [
+    (31, 8224, 32), (20, 9216, 128), (17, 8256, 64), (50, 2048, 1024), (4130, 288, 32), (4100, 192, 64), (4113, 640, 128),
+    (12300, 2048, 64)])
+def test_few_rows(m, n, k, group, x8):
+    """Rows that lanes share, a block's waves many and few, 16 to 64 outputs a wave."""
+    print(f"w4 m={m} n={n} k={k} group={group} x8={x8}", flush=True)
+    _check(*_data(m, n, k, group, BF if n % 2 else F16, x8, n % 3 != 0, seed=9))
+
+
+@pytest.mark.parametrize("m", [2, 4, 7])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_few_rows_do_not_touch_each_other(m, group):
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(m, 200, 896, group, BF, False, True)
+    clean = cp.w4_matvec(x, w, s, zero=z)
+    x[1, 7] = float("nan")
+    y = cp.w4_matvec(x, w, s, zero=z)
+    keep = [i for i in range(m) if i != 1]
+    assert torch.equal(y[keep], clean[keep])
+    assert bool(torch.isnan(y[1].float()).all())
