@@ -116,3 +116,23 @@ def test_products_near_the_ends_of_float32(xs, ws):
     scale = y.abs().amax(1) / 448.0
     ref.assert_close(got.scale[keep], scale[keep], F32, 2.0 ** -24 * 96 * scale[keep], "scale")
     ref.assert_e4m3(got.out.view(torch.uint8)[keep].view(got.out.dtype), (y / got.scale.cpu().double()[:, None])[keep], "codes")
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("t", [BF, F16, F32])
+@pytest.mark.parametrize("rows,d", [(9, 2), (5, 9), (17, 15), (40, 1001), (3, 8191), (4, 16385), (2, 40003), (2, 65535)])
+def test_rows_that_begin_anywhere(rows, d, t, quantize):
+    """d is no multiple of eight: no row but the first is aligned, every last run is short."""
+    import paper_2608_13226_amd as cp
+    print(f"norm rows={rows} d={d} {t} quantize={quantize}", flush=True)
+    x, w, r = _data(rows, d, t, True, seed=4)
+    # What lies around the outputs stays as it is.
+    e = torch.float8_e4m3fn if quantize else t
+    wide = torch.zeros(rows * d + 64, device="cuda", dtype=torch.uint8 if quantize else e)
+    wide.view(torch.uint8).fill_(0x55)
+    keep = torch.zeros(rows * d + 64, device="cuda", dtype=t)
+    keep.view(torch.uint8).fill_(0x55)
+    out = wide[:rows * d].view(e).view(rows, d)
+    got = cp.rms_norm(x, w, eps=1e-5, residual=r, quantize=quantize, out=out, residual_out=keep[:rows * d].view(rows, d))
+    _check(x, w, r, 1e-5, got, quantize)
+    assert bool((wide[rows * d:].view(torch.uint8) == 0x55).all()) and bool((keep[rows * d:].view(torch.uint8) == 0x55).all())
