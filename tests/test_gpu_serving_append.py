@@ -136,3 +136,14 @@ def test_a_cache_past_32_bits():
     cp.kv_append(None, k, v, torch.zeros(4, dtype=torch.int32, device="cuda"), slots, None, k_cache, v_cache)
     for i, s in enumerate(slots.tolist()):
         assert torch.equal(k_cache[s // page, :, s % page], k[i]) and torch.equal(v_cache[s // page, :, s % page], v[i])
+
+
+@pytest.mark.parametrize("c8", [False, True])
+@pytest.mark.parametrize("tokens,hq,hk,d,rot,page,interleaved,pad", [
+    (2051, 1, 1, 64, 64, 7, False, 0), (2053, 2, 2, 64, 16, 16, True, 0), (1031, 4, 1, 128, 64, 50, False, 0),
+    (2500, 3, 1, 96, 96, 128, False, 0), (2049, 2, 1, 36, 8, 16, True, 4), (4099, 1, 1, 7, 2, 5, False, 0),
+    (2061, 1, 1, 256, 256, 1, False, 1), (1030, 16, 4, 64, 32, 64, True, 0)])
+def test_many_tokens_of_few_heads(tokens, hq, hk, d, rot, page, interleaved, pad, c8):
+    """Blocks of several tokens, the last of them short, some tokens without a slot."""
+    print(f"append tokens={tokens} heads={hq}/{hk} d={d} rot={rot} page={page} c8={c8}", flush=True)
+    _run(tokens, hq, hk, d, rot, page, BF, E4M3 if c8 else BF, interleaved, pad=pad, drop=True)
