@@ -67,6 +67,11 @@ struct RawX {
       w = *reinterpret_cast<const u32x4*>(x + 2 * element);
     }
   }
+  // What another lane loaded.
+  __device__ __forceinline__ void take(int lane) {
+#pragma unroll
+    for (int e = 0; e < (X8 ? 2 : 4); ++e) w[e] = uint32_t(__builtin_amdgcn_ds_bpermute(4 * lane, int(w[e])));
+  }
   // Zero where !inside: the codes that meet it are another k's.
   template <class T>
   __device__ __forceinline__ u32x4 operand(bool inside = true) const {
@@ -108,6 +113,10 @@ __device__ __forceinline__ int group_of(const W4Params& p, int r) {
   return int(unsigned((uint64_t(r) * p.group_magic) >> 32) + unsigned(r) * p.group_one);
 }
 
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) {
+  return uint32_t(__builtin_amdgcn_ds_bpermute(4 * lane, int(v)));
+}
+
 // The scales and zero points of a lane's output.  A lane's load of two bytes
 // and one touches as many cache lines as one of its codes, so lane group g
 // loads those of the g-th of the next four groups that the wave meets (of SPAN
@@ -124,12 +133,11 @@ struct Scales {
     // Without zero points a byte of the scales is read in their place and dropped.
     z = ((p.zero ? p.zero : static_cast<const uint8_t*>(p.scale)) + base)[at];
   }
-  // What lane group d loaded -> all[d], of every lane.
-  __device__ __forceinline__ void trade(const W4Params& p, uint32_t* all) const {
+  // The d-th group's of output c, which lane 4 c + d has, -> all[d].
+  __device__ __forceinline__ void trade(const W4Params& p, int c, uint32_t* all) const {
     const uint32_t v = s | uint32_t(p.zero ? z : 8) << 16;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) all[d] = v;
-    transpose4(all);
+    for (int d = 0; d < 4; ++d) all[d] = from_lane(v, 4 * c + d);
   }
 };
 
@@ -140,10 +148,10 @@ __device__ __forceinline__ u32x4 load_codes(const W4Params& p, int64_t n0, unsig
   return *reinterpret_cast<const u32x4*>(base + (lane + unsigned(min(g * 32, p.k - 32 - at)) / 2));
 }
 
-template <class T, int SPAN>
+template <class T, bool TRADE>
 __device__ __forceinline__ void operands(u32x4 w, u32x4* a) {
   uint32_t v[4] = {w[0], w[1], w[2], w[3]};
-  if constexpr (SPAN < 4) transpose4(v);
+  if constexpr (TRADE) transpose4(v);
 #pragma unroll
   for (int j = 0; j < 4; ++j) a[j] = codes<T>(v[j]);
 }
@@ -181,6 +189,7 @@ __device__ __forceinline__ void spread(u32x4 v, u32x4* x) {
 template <class T, bool X8, int SPAN, int RT, int SHARE>
 __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p) {
   constexpr int kGroups = 4 / SPAN;
+  constexpr bool kDirect = SPAN == 4 && SHARE == 4;
   extern __shared__ float s_part[];               // [waves][RT][16][17]
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const int c = lane % 16, g = lane / 16;
@@ -190,14 +199,17 @@ __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Param
   const u32x4 ones = {one, one, one, one};
   unsigned row[RT];
 #pragma unroll
-  for (int i = 0; i < RT; ++i) row[i] = unsigned(min(int64_t(i * 16 + c), p.n - 1 - n0));
-  const unsigned xrow = unsigned(min(int64_t(c / SHARE), p.m - 1 - m0)) * unsigned(p.k);
+  for (int i = 0; i < RT; ++i) row[i] = unsigned(min(int64_t(i * 16 + lane / 4), p.n - 1 - n0));
+  const int own = 4 * c + g;                      // the lane that loads what this one needs
+  const unsigned xrow = unsigned(min(int64_t(kDirect ? c / SHARE : lane / (4 * SHARE)), p.m - 1 - m0)) * unsigned(p.k);
   const uint8_t* xbase = static_cast<const uint8_t*>(p.x) + m0 * p.k * (X8 ? 1 : 2);
   f32x4 y[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto k_of = [&](int kb, int j) { return kb + (SPAN < 4 ? j * 32 + g * 8 : g * 32 + j * 8); };
+  // Step j's k of this lane; the first of its j-th load of x.
+  auto k_of = [&](int kb, int j) { return kb + (kDirect ? g * 32 + j * 8 : j * 32 + g * 8); };
+  auto k_load = [&](int kb, int j) { return kDirect ? k_of(kb, c % SHARE) : kb + j * SHARE * 32 + lane % (4 * SHARE) * 8; };
   struct Stage {
     u32x4 w[RT];
     RawX<X8> x[4 / SHARE];
@@ -207,15 +219,15 @@ __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Param
   // What a run needs, on its way while the run before is worked on.
   auto load = [&](Stage& s, int kb) {
 #pragma unroll
-    for (int i = 0; i < RT; ++i) s.w[i] = load_codes(p, n0, row[i] * unsigned(p.k / 2), kb, g);
+    for (int i = 0; i < RT; ++i) s.w[i] = load_codes(p, n0, row[i] * unsigned(p.k / 2), kb, lane % 4);
 #pragma unroll
-    for (int j = 0; j < 4 / SHARE; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_of(kb, j * SHARE + c % SHARE), p.k - 8)));
+    for (int j = 0; j < 4 / SHARE; ++j) s.x[j].load(xbase, xrow + unsigned(min(k_load(kb, j), p.k - 8)));
     keep_loads_here();
   };
   auto load_scales = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < RT; ++i)
-      scales[i].load(p, n0, row[i] * unsigned(groups), groups, (kb + g / kGroups * step) / 32 + g % kGroups * SPAN);
+      scales[i].load(p, n0, row[i] * unsigned(groups), groups, (kb + lane % 4 / kGroups * step) / 32 + lane % kGroups * SPAN);
     keep_loads_here();
   };
   // Run t of SPAN at kb; all: their scales and zero points.
@@ -223,11 +235,15 @@ __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Param
     u32x4 a[RT][4], b[4];
     float sc[RT][kGroups], z[RT][kGroups];
 #pragma unroll
-    for (int j = 0; j < 4 / SHARE; ++j)
+    for (int j = 0; j < 4 / SHARE; ++j) {
+      if (!kDirect) s.x[j].take(own);
       spread<SHARE>(s.x[j].template operand<T>(SPAN == 4 || k_of(kb, j * SHARE + c % SHARE) < p.k), b + j * SHARE);
+    }
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      operands<T, SPAN>(s.w[i], a[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s.w[i][e] = from_lane(s.w[i][e], own);
+      operands<T, !kDirect>(s.w[i], a[i]);
 #pragma unroll
       for (int h = 0; h < kGroups; ++h) {
         const uint32_t v = all[i][t * kGroups + h];
@@ -262,7 +278,7 @@ __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Param
   while (kb < p.k) {
     uint32_t all[RT][4];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) scales[i].trade(p, all[i]);
+    for (int i = 0; i < RT; ++i) scales[i].trade(p, c, all[i]);
 #pragma unroll
     for (int t = 0; t < SPAN; ++t, kb += step) {
       if (kb >= p.k) break;
