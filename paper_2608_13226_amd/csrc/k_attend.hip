@@ -446,7 +446,7 @@ Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span) {
 
 // Tokens from the first one's tile on that a sequence can span.
 int64_t span_of(int64_t max_length, int64_t window) {
-  return window > 0 && window + kTile < max_length ? window + kTile : max_length;
+  return window > 0 && window < max_length - kTile ? window + kTile : max_length;
 }
 
 template <class T, bool C8, int D, int W, bool UNI>

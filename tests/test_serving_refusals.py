@@ -117,6 +117,14 @@ def test_attention_workspace(lib):
     assert size(1, 28, 4, 128, 131072, 32) == 0
 
 
+@pytest.mark.parametrize("window", [131072, 2 ** 31, 2 ** 62, 2 ** 63 - 33, 2 ** 63 - 32, 2 ** 63 - 1])
+def test_a_window_past_the_longest_length_is_none(lib, window):
+    """Any window of 64 bits: the workspace is that of the runs that are then written."""
+    size = lib.coverprune_paged_attention_workspace
+    assert size(1, 28, 4, 128, 131072, window) == size(1, 28, 4, 128, 131072, 0)
+    assert _attend(lib, width=10000, max_length=160000, window=window) == WORKSPACE
+
+
 def _t(*shape, dtype=torch.bfloat16):
     return torch.zeros(*shape, dtype=dtype)
 
