@@ -584,8 +584,8 @@ cp_status coverprune_kv_append(const void* q, int64_t q_stride, const void* k, i
  *               (entries outside [0, pages) are clamped; those that a length
  *               does not reach are not read)
  *   lengths     [batch] int32 tokens of each sequence, the new one included; 0
- *               gives o = 0 and lse = -inf.  Lengths over max_length count as
- *               max_length, negative ones as 0.
+ *               gives o = 0 and lse = -inf, as do scores that are all -inf.
+ *               Lengths over max_length count as max_length, negative ones as 0.
  *   max_length  the longest length, known to the host; 1 <= max_length <= width * page_size
  *   window      > 0: only the last `window` tokens count; 0: all
  *   scale       finite; 1 / sqrt(d) is the usual choice

@@ -2,7 +2,7 @@
 // split over the cache's length and joined:
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),
 // j over the sequence's tokens (the last `window` of them), m a running
-// maximum; o = 0 and lse = -inf where there is none.
+// maximum; o = 0 and lse = -inf where there is none, or no score above -inf.
 //
 // Bound by the cache's bytes: each key and value is read once, straight into
 // registers in the layout the matrix cores take, and serves all query heads
@@ -15,10 +15,12 @@
 //                 group loads the same contiguous dims of the group's eight
 //                 tokens; the operand's pairs (two tokens, one dim) are byte
 //                 permutations of its own registers, so V needs no LDS.
-// The running maximum moves only when a score passes it by more than 2^8, so
-// that the usual tile needs no exchange between lanes and no rescaling.
-// p is handed over as two values of the cache's type (its rounding and the
-// rest), so no accuracy is lost to it; sums and statistics are float32.
+// The running maximum moves only when a score passes it by more than 2^8 (2^4
+// with float16), so that the usual tile needs no exchange between lanes and no
+// rescaling.  p is handed over as two values of T (its rounding and the rest):
+// 16 bits and more of it, with bfloat16's range; with float16 p is 2^11 times as
+// large, so that what falls below its smallest value is under 2^-36 of the
+// largest p.  Sums and statistics are float32.
 #include <algorithm>
 #include <type_traits>
 
@@ -31,8 +33,12 @@ namespace {
 constexpr int kTile = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// How far a score may pass the running maximum, in powers of two.
-constexpr float kSlack = 8.f;
+// In powers of two: how far a score may pass the running maximum, and the
+// largest p until one does.  Their sum stays inside T's range.
+template <class T> constexpr float kSlack = 8.f;
+template <class T> constexpr float kLift = 0.f;
+template <> constexpr float kSlack<F16> = 4.f;
+template <> constexpr float kLift<F16> = 11.f;
 
 // 32 x 16 pieces of a head's dims held by a lane of the value operand: runs of
 // 8, 4 and 2 dims, from 128, 64 and 32 dims of the head.
@@ -185,6 +191,7 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   }
   const float to_log2 = p.scale * kLog2e * (p.k_scale ? p.k_scale[kh] : 1.f);
 
+  // m: log2 of the score whose p is 1, kLift below the running maximum.
   float m = -INFINITY, l = 0.f;
   f32x4 o[2 * L::pairs];
 #pragma unroll
@@ -253,20 +260,22 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-    if (__any(top > m + kSlack)) {
+    if (__any(top > m + (kSlack<T> + kLift<T>))) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float m2 = fmaxf(m, top);
+      const float m2 = fmaxf(m, top - kLift<T>);
       const float f = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m - m2);
       m = m2;
       l *= f;
 #pragma unroll
       for (int i = 0; i < 2 * L::pairs; ++i) o[i] *= f;
     }
+    // While no score is above -inf, each p is 0.
+    const float base = m == -INFINITY ? 0.f : m;
     u32x4 near, rest;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float a = __builtin_amdgcn_exp2f(x[i] - m), e = __builtin_amdgcn_exp2f(x[i + 1] - m);
+      const float a = __builtin_amdgcn_exp2f(x[i] - base), e = __builtin_amdgcn_exp2f(x[i + 1] - base);
       l += a + e;
       uint32_t n2, r2;
       split2<T>(a, e, n2, r2);

@@ -191,3 +191,46 @@ def test_the_same_answer_every_time_and_any_workspace():
         with pytest.raises(cp.CoverPruneError, match="workspace"):
             cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], max_length=9000,
                                workspace=ws[:need - 64])
+
+
+@pytest.mark.parametrize("c8", [False, True])
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("t", [F16, BF])
+def test_weights_far_below_the_largest(t, page, c8):
+    """A token of each 32 has exp(18) times the others' weight and no value: what the others give is the result."""
+    import paper_2608_13226_amd as cp
+    n, d = 64, 64
+    a = _data([n], 8, 2, d, page, t, E4M3 if c8 else t, garbage=False)
+    a["k_scale"] = a["v_scale"] = None
+    a["q"] = torch.ones_like(a["q"])
+    g = torch.Generator().manual_seed(5)
+    keys = torch.zeros(n, 1, 1).expand(n, 2, d).clone()
+    keys[5::32] = 18.0 / d
+    values = 200.0 + 200.0 * torch.rand(n, 2, d, generator=g)
+    values[5::32] = 0.0
+    at = torch.arange(n, device="cuda")
+    pages, off = a["table"][0].long()[at // page], at % page
+    c = a["k_cache"].dtype
+    for cache, x in ((a["k_cache"], keys), (a["v_cache"], values)):
+        cache.view(torch.uint8).view(*cache.shape[:3], -1)[pages, :, off] = x.to(c).cuda().view(torch.uint8)
+    out, lse = cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], scale=1.0, return_lse=True)
+    want, wlse, size = ref.attend(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], 0, 1.0)
+    # float16 holds a weight to 2^-36 of the largest; the rest is float32 work (bfloat16: two parts, 2^-16).
+    ref.assert_close(out, want, t, 2.0 ** -16 * size + n * 2.0 ** -36 * 448.0 * (t == F16), "out")
+    ref.assert_close(lse, wlse, torch.float32, 2.0 ** -18 * wlse.abs(), "lse")
+
+
+@pytest.mark.parametrize("t", [F16, BF])
+@pytest.mark.parametrize("shut", [0, 1, 32, 33, 64, 700, 3000])
+def test_scores_of_minus_infinity_count_nothing(shut, t):
+    """Keys that rule their tokens out, whole tiles and runs of them; the values there are ordinary."""
+    import paper_2608_13226_amd as cp
+    a = _data([3001, 0], 8, 2, 64, 16, t, t, garbage=False)
+    a["q"][:, :, 0] = 1.0
+    at = torch.arange(shut, device="cuda")
+    a["k_cache"][a["table"][0].long()[at // 16], :, at % 16, 0] = -math.inf
+    _check(a)
+    at = torch.arange(3001, device="cuda")
+    a["k_cache"][a["table"][0].long()[at // 16], :, at % 16, 0] = -math.inf
+    out, lse = cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], max_length=3001, return_lse=True)
+    assert not bool(out.any()) and bool(torch.isneginf(lse).all())
