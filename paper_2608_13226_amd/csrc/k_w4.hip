@@ -185,7 +185,8 @@ __device__ __forceinline__ void spread(u32x4 v, u32x4* x) {
 // / SHARE rows, SHARE neighbouring lanes hold one row: each loads its share of
 // the row's x once and they pass it on; row r of x is then the product's rows
 // SHARE r to SHARE r + SHARE - 1, all alike.  At 1 x 3584 x 28672, groups of
-// 128, 11.8 us (4.5 TB/s), at 16 rows 17.8 (3.0 TB/s).
+// 128, 15.0 us (3.5 TB/s) over weights that pass the caches, 11.8 where they
+// stay; at 16 rows 17.6 (3.0 TB/s) and 14.9.
 template <class T, bool X8, int SPAN, int RT, int SHARE>
 __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p) {
   constexpr int kGroups = 4 / SPAN;
@@ -525,35 +526,35 @@ hipError_t launch_few(const W4Params& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Which kernel (m rows; times of one call in a graph, k = 3584 and groups of
-// 128 where not said, us; a tile is 16 rows by 16 outputs):
+// Which kernel (rows x k x outputs, groups of 128, bf16; us of one call in a
+// graph, over weights that together pass the caches; a tile is 16 rows by 16
+// outputs):
 //   - more than 16 rows and many outputs: the wide one, whose time hardly
-//     depends on n up to a block a compute unit (64 rows: 29 at n = 4608, 30 at
-//     28672; 32 rows: 21 at 28672), while that of the other grows with it (64
-//     rows: 17 and 58; 32 rows: 10 and 31);
-//   - up to 4 rows, lanes share x four ways: 11.9 against 13.3 at n = 28672, 9.5
-//     against 10.7 at n = 3584, k = 14336; up to 8 rows, two ways: 12.8 against
-//     14.9, 10.4 against 15.3.  Shared four ways, more outputs a wave gain
-//     nothing (n = 4608: 4.8 and 4.7; 28672: 12.1 and 12.2);
-//   - 16 outputs a wave while there are fewer tiles than compute units (16 rows,
-//     n = 3584, k = 14336: 19 against 24 with 32); then 32 (n = 4608: 7.4
-//     against 10.2 with 16 and 10.3 with 64); and 64 when 32 would
-//     make more than a block a compute unit (32 rows, n = 4608: 10.6
-//     against 12.3; n = 28672, 16 rows: 17.8 against 22.1), or, where k is short
-//     and a block's start weighs, more than three (64 rows, n = 8000, k = 1024: 8.4
-//     against 10.2; but 48 rows 8.4 against 7.9);
+//     depends on n up to a block a compute unit, while that of the other grows
+//     with it (32x3584x28672 22.2 against 28.0, 64x3584x28672 33.0 against 46.6;
+//     but 32x2048x12000 13.8 against 9.2, 64x2048x12000 19.4 against 14.8: they
+//     meet near n = 16000);
+//   - up to 4 rows, lanes share x four ways (1x3584x4608 5.1 against 5.5 two ways
+//     and 6.0 with none, 1x14336x3584 9.2, 14.0 and 15.0); up to 8 rows, two ways
+//     (8x2048x12000 5.9 against 6.5 with none).  Shared four ways, more outputs
+//     a wave gain nothing (1x3584x28672 15.0 and 14.9);
+//   - 16 outputs a wave while there are fewer tiles than compute units
+//     (16x14336x3584 15.4, with 32 19.0); then 32 (16x3584x4608 6.2, with 16 7.1,
+//     with 64 10.5; 24x3584x4608 8.6, with 64 10.6; 48x14336x3584 26.6, with 64
+//     30.9); and 64 above three blocks of 32 a compute unit (16x3584x28672 17.5,
+//     with 32 19.1; 64x2048x12000 14.8 and 15.7; but 48x2048x12000 14.0 and 13.1);
 //   - 8 waves a block, 16 for a long k (one row, n = 3584, k = 14336: 8.4 against
 //     9.5; but n = 28672, k = 3584 14.1 against 12.1), 4 where each holds 64
 //     outputs.
 template <class T, bool X8, int SPAN>
 hipError_t launch_span(const W4Params& p, hipStream_t stream) {
-  if (p.m > 16 && p.n >= (p.m > 32 ? 8192 : 10240))
+  if (p.m > 16 && p.n >= 16384)
     return p.m <= 32 ? launch_wide<T, X8, SPAN, 2>(p, stream) : launch_wide<T, X8, SPAN, 4>(p, stream);
   const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
   if (p.m <= 4) return launch_few<T, X8, SPAN, 1, 4>(p, stream);
   if (p.m <= 8) return tiles < 256 ? launch_few<T, X8, SPAN, 1, 2>(p, stream) : launch_few<T, X8, SPAN, 2, 2>(p, stream);
   if (tiles < 256) return launch_few<T, X8, SPAN, 1, 1>(p, stream);
-  return tiles <= (p.k < 2048 ? 1536 : 512) ? launch_few<T, X8, SPAN, 2, 1>(p, stream) : launch_few<T, X8, SPAN, 4, 1>(p, stream);
+  return tiles <= 1536 ? launch_few<T, X8, SPAN, 2, 1>(p, stream) : launch_few<T, X8, SPAN, 4, 1>(p, stream);
 }
 
 template <class T, bool X8>

@@ -124,3 +124,25 @@ def test_few_rows_do_not_touch_each_other(m, group):
     keep = [i for i in range(m) if i != 1]
     assert torch.equal(y[keep], clean[keep])
     assert bool(torch.isnan(y[1].float()).all())
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("t", [BF, F16])
+@pytest.mark.parametrize("m,n,k,group", [
+    (17, 16390, 384, 128), (20, 16385, 160, 32), (33, 16400, 320, 32), (64, 16384, 1088, 64), (130, 16500, 1056, 96),
+    (40, 16387, 2304, 32), (64, 16641, 256, 256), (32, 16400, 32, 32)])
+def test_many_rows_and_outputs(m, n, k, group, t, x8):
+    """x shared in LDS: one block of rows and several, turns and groups that end anywhere."""
+    print(f"w4 m={m} n={n} k={k} group={group} {t} x8={x8}", flush=True)
+    _check(*_data(m, n, k, group, t, x8, n % 2 == 1, seed=4))
+
+
+def test_many_outputs_rows_do_not_touch_each_other():
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(20, 16500, 512, 128, BF, False, True)
+    clean = cp.w4_matvec(x, w, s, zero=z)
+    x[3, 7], x[18, 500] = float("nan"), float("inf")
+    y = cp.w4_matvec(x, w, s, zero=z)
+    keep = [i for i in range(20) if i not in (3, 18)]
+    assert torch.equal(y[keep], clean[keep])
+    assert not bool(torch.isfinite(y[3].float()).any())
