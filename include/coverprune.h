@@ -535,7 +535,7 @@ cp_status coverprune_rms_norm(const void* x, cp_dtype dtype, int64_t rows, int64
  *   group    a multiple of 32 that divides k (k <= 2^20)
  *   dtype    CP_BF16 or CP_F16
  *   y        [m, n], y_dtype == dtype or CP_F32
- * The time is that of reading the weights up to m = 16; every further 64 rows
+ * The time is that of reading the weights up to m = 16; every further 16 to 64 rows
  * read them again (from a cache, where they fit one).
  */
 cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_scale, const uint8_t* weight,

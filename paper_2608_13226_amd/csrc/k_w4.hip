@@ -530,10 +530,13 @@ hipError_t launch_few(const W4Params& p, hipStream_t stream) {
 // graph, over weights that together pass the caches; a tile is 16 rows by 16
 // outputs):
 //   - more than 16 rows and many outputs: the wide one, whose time hardly
-//     depends on n up to a block a compute unit, while that of the other grows
-//     with it (32x3584x28672 22.2 against 28.0, 64x3584x28672 33.0 against 46.6;
-//     but 32x2048x12000 13.8 against 9.2, 64x2048x12000 19.4 against 14.8: they
-//     meet near n = 16000);
+//     depends on either up to a block a compute unit, while that of the other
+//     grows with rows x outputs.  With 32 rows a block they meet near 655360
+//     (32x3584x28672 22.2 against 28.0, 64x3584x12288 20.6 against 21.8,
+//     64x1792x16384 13.2 against 16.8; but 32x3584x18000 21.5 against 20.9,
+//     48x3584x12288 20.2 against 18.3), while its blocks are not more than
+//     compute units; with 64 near 2^20 (64x3584x28672 33.0 against 46.6; but
+//     48x3584x18000 32.0 against 27.2);
 //   - up to 4 rows, lanes share x four ways (1x3584x4608 5.1 against 5.5 two ways
 //     and 6.0 with none, 1x14336x3584 9.2, 14.0 and 15.0); up to 8 rows, two ways
 //     (8x2048x12000 5.9 against 6.5 with none).  Shared four ways, more outputs
@@ -548,8 +551,11 @@ hipError_t launch_few(const W4Params& p, hipStream_t stream) {
 //     outputs.
 template <class T, bool X8, int SPAN>
 hipError_t launch_span(const W4Params& p, hipStream_t stream) {
-  if (p.m > 16 && p.n >= 16384)
-    return p.m <= 32 ? launch_wide<T, X8, SPAN, 2>(p, stream) : launch_wide<T, X8, SPAN, 4>(p, stream);
+  const int64_t work = (p.m + 15) / 16 * 16 * p.n;
+  if (p.m > 16 && work >= 655360) {
+    if (p.m <= 32 || (p.m + 31) / 32 * ((p.n + kWideRows - 1) / kWideRows) <= 256) return launch_wide<T, X8, SPAN, 2>(p, stream);
+    if (work >= 1 << 20) return launch_wide<T, X8, SPAN, 4>(p, stream);
+  }
   const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
   if (p.m <= 4) return launch_few<T, X8, SPAN, 1, 4>(p, stream);
   if (p.m <= 8) return tiles < 256 ? launch_few<T, X8, SPAN, 1, 2>(p, stream) : launch_few<T, X8, SPAN, 2, 2>(p, stream);

@@ -146,3 +146,26 @@ def test_many_outputs_rows_do_not_touch_each_other():
     keep = [i for i in range(20) if i not in (3, 18)]
     assert torch.equal(y[keep], clean[keep])
     assert not bool(torch.isfinite(y[3].float()).any())
+
+
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("m,n,k,group,t", [
+    (17, 20490, 384, 128, BF), (20, 20481, 160, 32, F16), (32, 20500, 32, 32, BF), (33, 13701, 1088, 64, F16),
+    (64, 10240, 2304, 32, BF), (64, 16384, 256, 256, F16), (64, 16385, 1056, 96, BF), (40, 22001, 320, 32, F16),
+    (130, 8300, 416, 32, BF), (99, 6001, 2176, 128, BF), (300, 4100, 192, 64, F16)])
+def test_rows_times_outputs(m, n, k, group, t, x8):
+    """32 and 64 rows a block, up to a block a compute unit and past it, last blocks of few rows and outputs."""
+    print(f"w4 m={m} n={n} k={k} group={group} {t} x8={x8}", flush=True)
+    _check(*_data(m, n, k, group, t, x8, n % 2 == 1, seed=6))
+
+
+@pytest.mark.parametrize("m,n", [(20, 20500), (64, 10300), (64, 17000)])
+def test_rows_times_outputs_do_not_touch_each_other(m, n):
+    import paper_2608_13226_amd as cp
+    x, w, s, z, _ = _data(m, n, 512, 128, BF, False, True)
+    clean = cp.w4_matvec(x, w, s, zero=z)
+    x[3, 7], x[18, 500] = float("nan"), float("inf")
+    y = cp.w4_matvec(x, w, s, zero=z)
+    keep = [i for i in range(m) if i not in (3, 18)]
+    assert torch.equal(y[keep], clean[keep])
+    assert not bool(torch.isfinite(y[3].float()).any())
