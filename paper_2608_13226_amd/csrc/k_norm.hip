@@ -120,7 +120,9 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
   float rms = 1.f / sqrtf(sq / float(p.d) + p.eps);
   if (!(sq > 1e-25f && sq < 1e37f)) {
     // Squares at the ends of float32's range: the same with h over a power of
-    // two near its largest.  (Nothing changes for zeros, infinities and NaN.)
+    // two near its largest.  (Nothing changes for zeros, infinities and NaN,
+    // nor where eps is so large beside the squares that they do not count:
+    // their sum over the power's square is below 2^18.)
     float scaled = 0.f;
     unsigned most = 0;
 #pragma unroll
@@ -138,7 +140,8 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
 #pragma unroll
           for (int e = 0; e < kRun; ++e) scaled = fmaf(h[v][e] * s, h[v][e] * s, scaled);
       row_reduce(scaled, most, s_sum[2], s_top[2]);
-      rms = s / sqrtf(scaled / float(p.d) + p.eps * s * s);
+      const float eps = p.eps * s * s;
+      if (eps < 1e30f) rms = s / sqrtf(scaled / float(p.d) + eps);
     }
   }
   if constexpr (!Q) {

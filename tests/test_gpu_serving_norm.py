@@ -136,3 +136,18 @@ def test_rows_that_begin_anywhere(rows, d, t, quantize):
     got = cp.rms_norm(x, w, eps=1e-5, residual=r, quantize=quantize, out=out, residual_out=keep[:rows * d].view(rows, d))
     _check(x, w, r, 1e-5, got, quantize)
     assert bool((wide[rows * d:].view(torch.uint8) == 0x55).all()) and bool((keep[rows * d:].view(torch.uint8) == 0x55).all())
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("size,eps", [(1e-13, 1e-6), (1e-19, 1e20), (1e-22, 1e-6), (1e-22, 1.0), (1e-25, 1e-6), (1e-25, 1e-5),
+                                      (1e-30, 1e-30), (1e-30, 1e-38), (1e-35, 1e-6), (1e-35, 1e-12), (1e-35, 1e-36)])
+def test_rows_far_below_the_root_of_eps(size, eps, t, quantize):
+    """eps alone under the root, or beside squares that float32 does not hold: small results, but not 0."""
+    import paper_2608_13226_amd as cp
+    x, w, r = _data(6, 1024, F32, True)
+    x, w, r = (x * size).to(t), w.to(t), (r * size).to(t)
+    # The kernel's eps is the nearest float32.
+    eps = float(torch.tensor(eps, dtype=F32))
+    _check(x, w, None, eps, cp.rms_norm(x, w, eps=eps, quantize=quantize), quantize)
+    _check(x, w, r, eps, cp.rms_norm(x, w, eps=eps, residual=r, quantize=quantize), quantize)
