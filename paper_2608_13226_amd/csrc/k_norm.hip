@@ -141,7 +141,21 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
           for (int e = 0; e < kRun; ++e) scaled = fmaf(h[v][e] * s, h[v][e] * s, scaled);
       row_reduce(scaled, most, s_sum[2], s_top[2]);
       const float eps = p.eps * s * s;
-      if (eps < 1e30f) rms = s / sqrtf(scaled / float(p.d) + eps);
+      if (eps < 1e30f) {
+        const float root = sqrtf(scaled / float(p.d) + eps);
+        rms = s / root;
+        if (rms > 3.4e38f) {
+          // 1 / rms itself is past float32: h over the power takes h's place, and
+          // 8 bits go step by step.
+          rms = 1.f / root;
+          top = 0;
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+            if ((v * int(blockDim.x) + int(threadIdx.x)) * kRun < p.d)
+#pragma unroll
+              for (int e = 0; e < kRun; ++e) h[v][e] *= s;
+        }
+      }
     }
   }
   if constexpr (!Q) {

@@ -151,3 +151,17 @@ def test_rows_far_below_the_root_of_eps(size, eps, t, quantize):
     eps = float(torch.tensor(eps, dtype=F32))
     _check(x, w, None, eps, cp.rms_norm(x, w, eps=eps, quantize=quantize), quantize)
     _check(x, w, r, eps, cp.rms_norm(x, w, eps=eps, residual=r, quantize=quantize), quantize)
+
+
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("t", [BF, F32])
+@pytest.mark.parametrize("size,eps", [(2e-39, 0.0), (3e-40, 0.0), (1e-40, 1e-45), (2e-39, 1e-38)])
+@pytest.mark.parametrize("d", [8, 1000, 40003])
+def test_subnormal_rows(d, size, eps, t, quantize):
+    """Rows whose 1 / rms float32 does not hold: results of the usual size."""
+    import paper_2608_13226_amd as cp
+    x, w, _ = _data(5, d, F32, False)
+    x, w = (x * size).to(t), w.to(t)
+    assert bool((x != 0).any(1).all())
+    eps = float(torch.tensor(eps, dtype=F32))
+    _check(x, w, None, eps, cp.rms_norm(x, w, eps=eps, quantize=quantize), quantize)
