@@ -17,8 +17,8 @@
 //                 permutations of its own registers, so V needs no LDS.
 // The running maximum moves only when a score passes it by more than 2^8 (2^4
 // with float16), so that the usual tile needs no exchange between lanes and no
-// rescaling.  p is handed over as two values of T (its rounding and the rest):
-// 16 bits and more of it, with bfloat16's range; with float16 p is 2^11 times as
+// rescaling.  p is handed over in parts of T that add up to it: three of
+// bfloat16 are all of its 24 bits; two of float16 are 22, with p 2^11 times as
 // large, so that what falls below its smallest value is under 2^-36 of the
 // largest p.  Sums and statistics are float32.
 #include <algorithm>
@@ -133,20 +133,26 @@ struct RawKey {
   }
 };
 
-// p as two values of T: one near it, and the rest.
+// Two p as packed pairs of T that add up to them, the largest part first.
+template <class T> constexpr int kParts = 3;
+template <> constexpr int kParts<F16> = 2;
 template <class T>
-__device__ __forceinline__ void split2(float a, float b, uint32_t& near, uint32_t& rest);
+__device__ __forceinline__ void split(float a, float b, uint32_t* part);
 template <>
-__device__ __forceinline__ void split2<Bf16>(float a, float b, uint32_t& near, uint32_t& rest) {
-  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-  near = __builtin_amdgcn_perm(y, x, 0x07060302u);
-  rest = pack2<Bf16>(a - __uint_as_float(x & 0xffff0000u), b - __uint_as_float(y & 0xffff0000u));
+__device__ __forceinline__ void split<Bf16>(float a, float b, uint32_t* part) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    part[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    a -= __uint_as_float(x & 0xffff0000u);
+    b -= __uint_as_float(y & 0xffff0000u);
+  }
 }
 template <>
-__device__ __forceinline__ void split2<F16>(float a, float b, uint32_t& near, uint32_t& rest) {
-  near = pack2<F16>(a, b);
-  const float2 r = unpack2<F16>(near);
-  rest = pack2<F16>(a - r.x, b - r.y);
+__device__ __forceinline__ void split<F16>(float a, float b, uint32_t* part) {
+  part[0] = pack2<F16>(a, b);
+  const float2 r = unpack2<F16>(part[0]);
+  part[1] = pack2<F16>(a - r.x, b - r.y);
 }
 
 // Loads above stay above: the compiler would move a load that the next turn of
@@ -272,15 +278,15 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     }
     // While no score is above -inf, each p is 0.
     const float base = m == -INFINITY ? 0.f : m;
-    u32x4 near, rest;
+    u32x4 part[kParts<T>];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float a = __builtin_amdgcn_exp2f(x[i] - base), e = __builtin_amdgcn_exp2f(x[i + 1] - base);
       l += a + e;
-      uint32_t n2, r2;
-      split2<T>(a, e, n2, r2);
-      near[i / 2] = n2;
-      rest[i / 2] = r2;
+      uint32_t w[kParts<T>];
+      split<T>(a, e, w);
+#pragma unroll
+      for (int n = 0; n < kParts<T>; ++n) part[n][i / 2] = w[n];
     }
 #pragma unroll
     for (int i = 0; i < L::pairs; ++i) {
@@ -291,10 +297,11 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
         even[j] = __builtin_amdgcn_perm(e, a, 0x05040100u);
         odd[j] = __builtin_amdgcn_perm(e, a, 0x07060302u);
       }
-      o[2 * i] = mfma32<T>(even, near, o[2 * i]);
-      o[2 * i + 1] = mfma32<T>(odd, near, o[2 * i + 1]);
-      o[2 * i] = mfma32<T>(even, rest, o[2 * i]);
-      o[2 * i + 1] = mfma32<T>(odd, rest, o[2 * i + 1]);
+#pragma unroll
+      for (int n = 0; n < kParts<T>; ++n) {
+        o[2 * i] = mfma32<T>(even, part[n], o[2 * i]);
+        o[2 * i + 1] = mfma32<T>(odd, part[n], o[2 * i + 1]);
+      }
     }
     if (more) load_values(next);
   };

@@ -234,3 +234,32 @@ def test_scores_of_minus_infinity_count_nothing(shut, t):
     a["k_cache"][a["table"][0].long()[at // 16], :, at % 16, 0] = -math.inf
     out, lse = cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], max_length=3001, return_lse=True)
     assert not bool(out.any()) and bool(torch.isneginf(lse).all())
+
+
+@pytest.mark.parametrize("c8", [False, True])
+@pytest.mark.parametrize("t", [F16, BF])
+@pytest.mark.parametrize("n,d,page", [(2, 64, 16), (2, 128, 32), (64, 96, 50), (700, 128, 64), (900, 192, 16)])
+def test_weights_keep_float32s_bits(n, d, page, t, c8):
+    """Values of 1 and -1 in turn under nearly equal weights: what is left of their sum shows the weights' last bits."""
+    import paper_2608_13226_amd as cp
+    a = _data([n] * 32, 28, 4, d, page, t, E4M3 if c8 else t, garbage=False)
+    a["k_scale"] = a["v_scale"] = None
+    g = torch.Generator(device="cuda").manual_seed(n + d)
+    a["q"].zero_()
+    a["q"][:, :, 0] = 1.0 + torch.rand(32, 28, device="cuda", generator=g).to(t)
+    c = a["k_cache"].dtype
+    at = torch.arange(n, device="cuda")
+    keys = torch.zeros(n, 4, d, device="cuda")
+    keys[:, :, 0] = torch.randint(1, 8, (n, 4), device="cuda", generator=g) * 2.0 ** -9
+    keys[1, :, 0] = 0.0
+    values = (1.0 - 2.0 * (at % 2))[:, None, None].expand(n, 4, d)
+    for b in range(32):
+        pages, off = a["table"][b].long()[at // page], at % page
+        for cache, x in ((a["k_cache"], keys), (a["v_cache"], values)):
+            cache.view(torch.uint8).view(*cache.shape[:3], -1)[pages, :, off] = x.contiguous().to(c).view(torch.uint8)
+    scale = 2.0 ** -6
+    out = cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], max_length=n, scale=scale)
+    want, _, size = ref.attend(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], 0, scale)
+    # Scores below 2^-10, so a weight is an exponential's 2^-23 off and no more; sums of n / 32 steps a wave, at
+    # most 2^-24 (n / 128 + 8) of the summands' size.
+    ref.assert_close(out, want, t, 2.0 ** -20 * size, "out")
