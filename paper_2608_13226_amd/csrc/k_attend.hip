@@ -133,7 +133,11 @@ struct RawKey {
   }
 };
 
-// Two p as packed pairs of T that add up to them, the largest part first.
+// Two p as packed pairs of T that add up to them, the largest part first.  An
+// infinite value has to meet no part of another sign and, while p is not 0, no
+// part of 0: bfloat16's parts are cut below what they are parts of, so that
+// there is always a rest (p from 2^-90 on), and a float16 p's rest meets the
+// values through finite2.
 template <class T> constexpr int kParts = 3;
 template <> constexpr int kParts<F16> = 2;
 template <class T>
@@ -141,18 +145,27 @@ __device__ __forceinline__ void split(float a, float b, uint32_t* part);
 template <>
 __device__ __forceinline__ void split<Bf16>(float a, float b, uint32_t* part) {
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  for (int i = 0; i < 2; ++i) {
+    // The float below, or 0.
+    const uint32_t x = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), y = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
     part[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
     a -= __uint_as_float(x & 0xffff0000u);
     b -= __uint_as_float(y & 0xffff0000u);
   }
+  part[2] = pack2<Bf16>(a, b);
 }
 template <>
 __device__ __forceinline__ void split<F16>(float a, float b, uint32_t* part) {
   part[0] = pack2<F16>(a, b);
   const float2 r = unpack2<F16>(part[0]);
   part[1] = pack2<F16>(a - r.x, b - r.y);
+}
+// A packed pair of float16 with infinities as the largest numbers.  (NaN may
+// become one too; the largest part of p meets the pair as it is.)
+__device__ __forceinline__ uint32_t finite2(uint32_t w) {
+  const f16x2 most = {(_Float16)65504.f, (_Float16)65504.f};
+  const f16x2 v = __builtin_elementwise_max(__builtin_elementwise_min(__builtin_bit_cast(f16x2, w), most), -most);
+  return __builtin_bit_cast(uint32_t, v);
 }
 
 // Loads above stay above: the compiler would move a load that the next turn of
@@ -299,6 +312,13 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
       }
 #pragma unroll
       for (int n = 0; n < kParts<T>; ++n) {
+        if (std::is_same_v<T, F16> && !C8 && n == 1) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            even[j] = finite2(even[j]);
+            odd[j] = finite2(odd[j]);
+          }
+        }
         o[2 * i] = mfma32<T>(even, part[n], o[2 * i]);
         o[2 * i + 1] = mfma32<T>(odd, part[n], o[2 * i + 1]);
       }

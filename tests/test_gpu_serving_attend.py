@@ -263,3 +263,32 @@ def test_weights_keep_float32s_bits(n, d, page, t, c8):
     # Scores below 2^-10, so a weight is an exponential's 2^-23 off and no more; sums of n / 32 steps a wave, at
     # most 2^-24 (n / 128 + 8) of the summands' size.
     ref.assert_close(out, want, t, 2.0 ** -20 * size, "out")
+
+
+@pytest.mark.parametrize("t", [F16, BF])
+@pytest.mark.parametrize("lengths,hq,hk,d,page", [([1, 2], 4, 2, 64, 16), ([33, 5], 28, 4, 128, 50), ([700, 1500], 8, 2, 96, 32),
+                                                  ([4000], 6, 1, 256, 64)])
+def test_infinite_values_among_the_tokens(lengths, hq, hk, d, page, t):
+    """An infinite value makes its dimension infinite, two of both signs NaN; all else stays."""
+    a = _data(lengths, hq, hk, d, page, t, t, seed=2)
+    for b, n in enumerate(lengths):
+        for i, (at, dim, value) in enumerate([(0, 3, math.inf), (n - 1, 7, -math.inf), (n // 2, d - 1, math.inf),
+                                              (0, 20, math.inf), (n - 1, 20, -math.inf if n > 1 else math.inf)]):
+            a["v_cache"][int(a["table"][b, at // page]), i % hk, at % page, dim] = value
+            if i >= 3:
+                a["v_cache"][int(a["table"][b, at // page]), :, at % page, dim] = value
+    out, _ = _check(a)
+    assert bool(torch.isinf(out).any()) and bool(torch.isnan(out).any()) == (max(lengths) > 1)
+
+
+@pytest.mark.parametrize("t", [F16, BF])
+def test_one_token_is_its_value(t):
+    """The only token's weight is 1, whatever its value."""
+    import paper_2608_13226_amd as cp
+    a = _data([1], 8, 2, 64, 16, t, t)
+    row = a["v_cache"][int(a["table"][0, 0]), :, 0]
+    row[0, :6] = torch.tensor([math.inf, -math.inf, math.nan, torch.finfo(t).max, torch.finfo(t).min, torch.finfo(t).tiny], dtype=t)
+    out = cp.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["table"], a["lengths"], max_length=1)
+    want = row.repeat_interleave(4, 0)[None]
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(out), nan) and torch.equal(out[~nan], want[~nan])
