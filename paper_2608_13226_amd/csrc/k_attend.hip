@@ -34,9 +34,10 @@ constexpr int kTile = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // In powers of two: how far a score may pass the running maximum, and the
-// largest p until one does.  Their sum stays inside T's range.
+// largest p until one does.  Their sum stays inside T's range, and with bfloat16
+// no p passes 1, so that values near the ends of its range stay inside float32.
 template <class T> constexpr float kSlack = 8.f;
-template <class T> constexpr float kLift = 0.f;
+template <class T> constexpr float kLift = -8.f;
 template <> constexpr float kSlack<F16> = 4.f;
 template <> constexpr float kLift<F16> = 11.f;
 

@@ -292,3 +292,21 @@ def test_one_token_is_its_value(t):
     want = row.repeat_interleave(4, 0)[None]
     nan = torch.isnan(want)
     assert torch.equal(torch.isnan(out), nan) and torch.equal(out[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("n", [280, 5000])
+def test_values_near_the_end_of_float32(n):
+    """Two tokens of a wave, the later one's weight 148 times the first's: no sum passes float32's range."""
+    a = _data([n], 8, 2, 128, 16, BF, BF, garbage=False)
+    a["q"] = torch.ones_like(a["q"])
+    at = torch.arange(n, device="cuda")
+    pages, off = a["table"][0].long()[at // 16], at % 16
+    keys = torch.full((n, 2, 128), -0.25, device="cuda")
+    values = torch.ones(n, 2, 128, device="cuda")
+    for at, score, value in ((3, 0.0, 1e38), (260, 5.0, 2e38)):
+        keys[at], values[at] = 0.0, value
+        keys[at, :, 0] = score
+    for cache, x in ((a["k_cache"], keys), (a["v_cache"], values)):
+        cache[pages, :, off] = x.to(BF)
+    out, _ = _check(a, scale=1.0)
+    assert bool(torch.isfinite(out).all())
