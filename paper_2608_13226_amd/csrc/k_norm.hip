@@ -174,8 +174,10 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
     const float most = __uint_as_float(top);
     float scale = most * rms / kE4m3Max;
     if (most > 1e-30f && most < 1e30f && scale > 1e-30f) {
-      // One division a row; no product passes 448 by more than float32's rounding.
-      const float factor = kE4m3Max / most;
+      // One division a row, whose quotient is kept in two parts so that a code is
+      // that of h w / (most / 448) to float32's last bit; no product passes 448 by
+      // more than float32's rounding.
+      const float factor = kE4m3Max / most, rest = fmaf(-factor, most, kE4m3Max) / most;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int j = (v * int(blockDim.x) + int(threadIdx.x)) * kRun;
@@ -183,7 +185,10 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
           float w[kRun];
           load_run<T, ANY>(p.weight, j, p.d - j, w);
 #pragma unroll
-          for (int e = 0; e < kRun; ++e) h[v][e] = h[v][e] * w[e] * factor;
+          for (int e = 0; e < kRun; ++e) {
+            const float y = h[v][e] * w[e];
+            h[v][e] = fmaf(y, factor, y * rest);
+          }
           uint8_t* out = static_cast<uint8_t*>(p.out) + base + j;
           const u32x2 codes = {pack4_e4m3_inside(h[v][0], h[v][1], h[v][2], h[v][3]),
                                pack4_e4m3_inside(h[v][4], h[v][5], h[v][6], h[v][7])};

@@ -165,3 +165,23 @@ def test_subnormal_rows(d, size, eps, t, quantize):
     assert bool((x != 0).any(1).all())
     eps = float(torch.tensor(eps, dtype=F32))
     _check(x, w, None, eps, cp.rms_norm(x, w, eps=eps, quantize=quantize), quantize)
+
+
+@pytest.mark.parametrize("t", [BF, F16, F32])
+@pytest.mark.parametrize("d", [200, 3584, 5001])
+def test_codes_half_way_between_two(t, d):
+    """Rows of n / 2 (n a whole number) times a row's factor, the largest 448 times it: half-way values go to the even code."""
+    import paper_2608_13226_amd as cp
+    g = torch.Generator(device="cuda").manual_seed(d)
+    rows = 64
+    # The factor's bits and the values' fill the type's.
+    bits = {BF: 3, F16: 6, F32: 19}[t]
+    m = 2.0 * torch.randint(0, 2 ** (bits - 1), (rows, 1), device="cuda", generator=g) + 1.0
+    n = torch.randint(0, 32, (rows, d), device="cuda", generator=g).float()
+    sign = 1.0 - 2.0 * torch.randint(0, 2, (rows, d), device="cuda", generator=g)
+    want = n * 2.0 ** torch.randint(-3, 4, (rows, d), device="cuda", generator=g) * sign
+    want[:, d // 3] = 448.0
+    x = want * m * 2.0 ** -4
+    assert torch.equal(x.to(t).float(), x)
+    got = cp.rms_norm(x.to(t), torch.ones(d, device="cuda", dtype=t), quantize=True)
+    assert torch.equal(got.out.float(), want.to(torch.float8_e4m3fn).float())
