@@ -99,6 +99,27 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// One y (without x's scale) as the formula says, code by code.  The kernels take
+// the zero points off the groups' sums, which is another thing where x is
+// infinite, or a sum past float32's range; such results are found again here.
+template <class T>
+__device__ __forceinline__ float by_formula(const W4Params& p, int64_t m, int64_t n) {
+  const int groups = p.k / p.group;
+  float y = 0.f;
+  for (int i = 0; i < groups && y == y; ++i) {
+    const float zero = p.zero ? float(p.zero[n * groups + i]) : 8.f;
+    float sum = 0.f;
+    for (int j = i * p.group; j < (i + 1) * p.group; j += 2) {
+      const int two = p.weight[n * (p.k / 2) + j / 2];
+      sum = fmaf(load1<T>(p.x, m * p.k + j), float(two & 15) - zero, sum);
+      sum = fmaf(load1<T>(p.x, m * p.k + j + 1), float(two >> 4) - zero, sum);
+    }
+    y = fmaf(sum, load1<T>(p.scale, n * groups + i), y);
+  }
+  return y;
+}
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+
 // SPAN: steps of 32 k between two groups' ends, 4, 2 or 1 (group a multiple of
 // 128, of 64, of 32).
 //
@@ -300,6 +321,7 @@ __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Param
     float v = 0.f;
     for (int x = 0; x < waves; ++x) v += s_part[((x * RT + i) * 16 + mr) * 17 + e % 16];
     if (X8) v *= p.x_scale[m];
+    else if (!is_finite(v)) v = by_formula<T>(p, m, n);
     if (p.y_type == ServeType::kF32) store1<F32>(p.y, m * p.n + n, v);
     else store1<T>(p.y, m * p.n + n, v);
   }
@@ -496,6 +518,11 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
   __syncthreads();
   if (half == 1) return;
   const int64_t n = out0 + c;
+  auto store = [&](int64_t m, float v) {
+    if (p.y_type == ServeType::kF32) store1<F32>(p.y, m * p.n + n, v);
+    else store1<T>(p.y, m * p.n + n, v);
+  };
+  unsigned again = 0;                             // bit 4 t + r
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const f32x4 o = part[t * kWave];
@@ -505,9 +532,14 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
       if (m >= p.m || n >= p.n) continue;
       float v = y[t][r] + o[r];
       if (X8) v *= p.x_scale[m];
-      if (p.y_type == ServeType::kF32) store1<F32>(p.y, m * p.n + n, v);
-      else store1<T>(p.y, m * p.n + n, v);
+      else again |= unsigned(!is_finite(v)) << (4 * t + r);
+      store(m, v);
     }
+  }
+  for (; !X8 && again; again &= again - 1) {
+    const int i = __builtin_ctz(again);
+    const int64_t m = m0 + i / 4 * 16 + g * 4 + i % 4;
+    store(m, by_formula<T>(p, m, n));
   }
 }
 

@@ -169,3 +169,33 @@ def test_rows_times_outputs_do_not_touch_each_other(m, n):
     keep = [i for i in range(m) if i not in (3, 18)]
     assert torch.equal(y[keep], clean[keep])
     assert not bool(torch.isfinite(y[3].float()).any())
+
+
+@pytest.mark.parametrize("t", [BF, F16])
+@pytest.mark.parametrize("zero", [False, True])
+@pytest.mark.parametrize("m,n,k,group", [(1, 40, 8320, 64), (3, 200, 896, 128), (7, 90, 320, 32), (20, 100, 512, 128), (40, 5000, 384, 96),
+                                         (20, 20500, 512, 128), (64, 16700, 288, 32)])
+def test_rows_with_infinities(m, n, k, group, zero, t):
+    """An infinite x gives infinity of the sign of code - zero, NaN where that is 0 or two of them disagree; a sum of
+    large x that float32 does not hold counts as the formula has it."""
+    print(f"w4 infinities m={m} n={n} k={k} group={group} {t} zero={zero}", flush=True)
+    x, w, s, z, _ = _data(m, n, k, group, t, False, zero, seed=11)
+    inf = float("inf")
+    x[0, 5] = inf
+    if m > 1:
+        x[m - 1, k - 1] = -inf
+    if m > 2:
+        x[1, 7], x[1, k // 2] = inf, -inf
+    if m > 5:
+        # Four large x of one sign at codes one above and one below the zero point.
+        x[3, 0:4] = 1.5e38 if t == BF else 6e4
+        at = torch.full((n,), 8, device="cuda", dtype=torch.uint8) if z is None else z[:, 0].clamp(1, 14)
+        if z is not None:
+            z[:, 0] = at
+        w[:, 0] = (at + 1) | (at - 1) << 4
+        w[:, 1] = (at - 1) | (at + 1) << 4
+    for out_dtype in (None, F32):
+        y = _check(x, w, s, z, None, out_dtype=out_dtype)
+        assert bool(torch.isinf(y[0].float()).any()) and bool(torch.isnan(y[0].float()).any() == ((w[:, 2] >> 4) == (8 if z is None else z[:, 0])).any())
+        if m > 5:
+            assert bool(torch.isfinite(y[3].float()).all())
