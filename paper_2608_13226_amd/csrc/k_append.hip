@@ -44,10 +44,10 @@ __device__ __forceinline__ void store_run(void* p, int64_t i, float* x, float de
 // when interleaved); VEC = 4 half of each; VEC = 1 is for everything else.
 // A block of 256 has `threads` for each of its tokens.
 template <class T, class C, int VEC, bool INTER>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int threads) {
+__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendParams p, int threads, int64_t first_block) {
   extern __shared__ float s_turns[];          // a token's [rot / 2] cosines, [rot / 2] sines
   const int tid = threadIdx.x % threads, mine = threadIdx.x / threads;
-  const int64_t token = int64_t(blockIdx.x) * (256 / threads) + mine, t = min(token, p.tokens - 1);
+  const int64_t token = (first_block + blockIdx.x) * (256 / threads) + mine, t = min(token, p.tokens - 1);
   float* s_turn = s_turns + mine * p.rot;
   const int half = p.rot / 2;
   // All that is read before the angles is on its way together.  (The values
@@ -149,9 +149,9 @@ hipError_t launch(const KvAppendParams& p, hipStream_t stream) {
   int threads = 256;
   while (threads > 32 && threads / 2 >= work / 4 && p.tokens * (threads / 2) >= 256 * 256) threads /= 2;
   const int64_t per = 256 / threads;
-  kv_append_kernel<T, C, VEC, INTER><<<dim3(unsigned((p.tokens + per - 1) / per), y), dim3(256), size_t(per) * p.rot * sizeof(float),
-                                       stream>>>(p, threads);
-  return hipGetLastError();
+  return launch_blocks((p.tokens + per - 1) / per, 256, [&](int64_t first, unsigned blocks) {
+    kv_append_kernel<T, C, VEC, INTER><<<dim3(blocks, y), dim3(256), size_t(per) * p.rot * sizeof(float), stream>>>(p, threads, first);
+  });
 }
 
 bool aligned(const void* q, int64_t stride, int bytes) {

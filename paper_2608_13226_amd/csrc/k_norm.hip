@@ -75,10 +75,10 @@ __device__ __forceinline__ void store_run(void* p, int64_t i, int left, const fl
 }
 
 template <class T, bool Q, bool ANY, int NV>
-__global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p) {
+__global__ __launch_bounds__(1024) void rms_norm_kernel(RmsNormParams p, int64_t first) {
   __shared__ float s_sum[4][16];
   __shared__ unsigned s_top[4][16];
-  const int64_t row = blockIdx.x;
+  const int64_t row = first + blockIdx.x;
   const int64_t base = row * p.d;
   float h[NV][kRun];
   float sq = 0.f;
@@ -239,12 +239,13 @@ hipError_t launch(const RmsNormParams& p, hipStream_t stream) {
   const int runs = (p.d + kRun - 1) / kRun;
   const int threads = runs >= 1024 ? 1024 : (runs + kWave - 1) / kWave * kWave;
   const int nv = (runs + threads - 1) / threads;
-  const dim3 grid(unsigned(p.rows)), block(threads);
-  if (nv <= 1) rms_norm_kernel<T, Q, ANY, 1><<<grid, block, 0, stream>>>(p);
-  else if (nv <= 2) rms_norm_kernel<T, Q, ANY, 2><<<grid, block, 0, stream>>>(p);
-  else if (nv <= 4) rms_norm_kernel<T, Q, ANY, 4><<<grid, block, 0, stream>>>(p);
-  else rms_norm_kernel<T, Q, ANY, 8><<<grid, block, 0, stream>>>(p);
-  return hipGetLastError();
+  return launch_blocks(p.rows, threads, [&](int64_t first, unsigned rows) {
+    const dim3 grid(rows), block(threads);
+    if (nv <= 1) rms_norm_kernel<T, Q, ANY, 1><<<grid, block, 0, stream>>>(p, first);
+    else if (nv <= 2) rms_norm_kernel<T, Q, ANY, 2><<<grid, block, 0, stream>>>(p, first);
+    else if (nv <= 4) rms_norm_kernel<T, Q, ANY, 4><<<grid, block, 0, stream>>>(p, first);
+    else rms_norm_kernel<T, Q, ANY, 8><<<grid, block, 0, stream>>>(p, first);
+  });
 }
 
 template <class T, bool Q>

@@ -209,13 +209,13 @@ __device__ __forceinline__ void spread(u32x4 v, u32x4* x) {
 // 128, 15.0 us (3.5 TB/s) over weights that pass the caches, 11.8 where they
 // stay; at 16 rows 17.6 (3.0 TB/s) and 14.9.
 template <class T, bool X8, int SPAN, int RT, int SHARE>
-__global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p) {
+__global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p, int64_t first_block) {
   constexpr int kGroups = 4 / SPAN;
   constexpr bool kDirect = SPAN == 4 && SHARE == 4;
   extern __shared__ float s_part[];               // [waves][RT][16][17]
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
   const int c = lane % 16, g = lane / 16;
-  const int64_t n0 = int64_t(blockIdx.x) * (16 * RT), m0 = int64_t(blockIdx.y) * 16;
+  const int64_t n0 = (first_block + blockIdx.x) * (16 * RT), m0 = int64_t(blockIdx.y) * 16;
   const int groups = p.k / p.group;
   const uint32_t one = pack2<T>(1.f, 1.f);
   const u32x4 ones = {one, one, one, one};
@@ -383,7 +383,7 @@ __device__ __forceinline__ float add2<F16>(uint32_t w, float c) {
 constexpr int kWideRows = 128;
 constexpr int kWideGroups = 64;                   // whose scales are in LDS at a time
 template <class T, bool X8, int SPAN, int MT>
-__global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
+__global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p, int64_t first_block) {
   constexpr int kGroups = 4 / SPAN, kPitch = kWideGroups + 2, kMine = MT / 2;
   __shared__ u32x4 s_x[2][2][4][MT][kWave];       // [turn % 2][half][step][row tile][lane]
   __shared__ uint16_t s_scale[kWideRows * kPitch];
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
   __shared__ float s_sum[2][2][MT][kWave];        // [turn % 2][half][row tile][group, row]
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c = lane % 16, g = lane / 16, half = wave / 8;
-  const int64_t first = int64_t(blockIdx.x) * kWideRows, out0 = first + wave % 8 * 16, n0 = min(out0, p.n - 1);
+  const int64_t first = (first_block + blockIdx.x) * kWideRows, out0 = first + wave % 8 * 16, n0 = min(out0, p.n - 1);
   const int64_t m0 = int64_t(blockIdx.y) * (16 * MT);
   const int turns = (p.k + 255) / 256, last_group = p.k / p.group - 1;
   const unsigned row = unsigned(min(int64_t(c), p.n - 1 - n0)) * unsigned(p.k / 2);
@@ -545,17 +545,20 @@ __global__ __launch_bounds__(1024) void w4_wide_kernel(W4Params p) {
 
 template <class T, bool X8, int SPAN, int MT>
 hipError_t launch_wide(const W4Params& p, hipStream_t stream) {
-  const dim3 grid(unsigned((p.n + kWideRows - 1) / kWideRows), unsigned((p.m + 16 * MT - 1) / (16 * MT)));
-  w4_wide_kernel<T, X8, SPAN, MT><<<grid, dim3(1024), 0, stream>>>(p);
-  return hipGetLastError();
+  const unsigned row_blocks = unsigned((p.m + 16 * MT - 1) / (16 * MT));
+  return launch_blocks((p.n + kWideRows - 1) / kWideRows, 1024, [&](int64_t first, unsigned blocks) {
+    w4_wide_kernel<T, X8, SPAN, MT><<<dim3(blocks, row_blocks), dim3(1024), 0, stream>>>(p, first);
+  });
 }
 
 template <class T, bool X8, int SPAN, int RT, int SHARE>
 hipError_t launch_few(const W4Params& p, hipStream_t stream) {
   const int most = RT == 4 ? 4 : SHARE == 4 && p.k >= 8192 ? 16 : 8, waves = std::min(most, (p.k + 127) / 128);
-  const dim3 grid(unsigned((p.n + 16 * RT - 1) / (16 * RT)), unsigned((p.m + 15) / 16));
-  w4_few_kernel<T, X8, SPAN, RT, SHARE><<<grid, dim3(kWave * waves), size_t(waves) * RT * 272 * sizeof(float), stream>>>(p);
-  return hipGetLastError();
+  const unsigned row_blocks = unsigned((p.m + 15) / 16);
+  return launch_blocks((p.n + 16 * RT - 1) / (16 * RT), kWave * waves, [&](int64_t first, unsigned blocks) {
+    w4_few_kernel<T, X8, SPAN, RT, SHARE><<<dim3(blocks, row_blocks), dim3(kWave * waves), size_t(waves) * RT * 272 * sizeof(float),
+                                            stream>>>(p, first);
+  });
 }
 
 // Which kernel (rows x k x outputs, groups of 128, bf16; us of one call in a

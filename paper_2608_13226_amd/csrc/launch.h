@@ -196,6 +196,20 @@ size_t lite_workspace_bytes(int64_t n, int64_t k);
 hipError_t launch_lite(const LiteParams& p, hipStream_t stream);
 
 // The serving operators.
+
+// HIP launches less than 2^32 work items a dimension.  A grid of `blocks` blocks
+// of `threads` in as many launches as that takes: launch(first block, blocks).
+template <class F>
+hipError_t launch_blocks(int64_t blocks, int threads, F launch) {
+  const int64_t most = ((int64_t(1) << 32) - 1) / threads;
+  for (int64_t first = 0; first < blocks; first += most) {
+    launch(first, unsigned(blocks - first < most ? blocks - first : most));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 enum class ServeType { kBf16, kF16, kF32, kE4m3 };
 
 struct RmsNormParams {
