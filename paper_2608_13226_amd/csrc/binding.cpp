@@ -10,6 +10,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 
 #include <cmath>
@@ -44,9 +45,13 @@ void check(cp_status st) {
   if (st != CP_OK) raise(g_error, "%s: %s", coverprune_status_string(st), coverprune_last_error());
 }
 
+// The operators have no backward pass: what they would cut from a graph is refused.
 const Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) raise(PyExc_TypeError, "%s must be a torch.Tensor", name);
-  return THPVariable_Unpack(o);
+  const Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && at::GradMode::is_enabled())
+    raise(PyExc_ValueError, "%s requires a gradient, which this operator does not give: detach it, or call under torch.no_grad()", name);
+  return t;
 }
 
 // A tensor argument that may be None (an undefined tensor then).

@@ -8,7 +8,8 @@ current GPU, enqueues on torch's current stream (or ``stream``) and returns
 without waiting; outputs that are not given are allocated.  8-bit tensors are
 torch.float8_e4m3fn throughout.  Wrong types raise TypeError, wrong shapes,
 strides and devices ValueError, what the library itself refuses
-CoverPruneError.
+CoverPruneError.  There are no backward passes: tensors that require a gradient
+raise ValueError, except under torch.no_grad().
 """
 from __future__ import annotations
 

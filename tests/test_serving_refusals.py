@@ -189,3 +189,36 @@ def test_binding_refuses():
         cp.paged_attention(*good, max_length=32)
     with pytest.raises(ValueError, match="GPU"):
         cp.rms_norm(_t(4, 64), w)
+
+
+def _calls():
+    """Each operator with its tensors by name, on the CPU and otherwise in order."""
+    import paper_2608_13226_amd as cp
+    f32, e4m3 = torch.float32, torch.float8_e4m3fn
+    q, k, cache = _t(3, 8, 128), _t(3, 2, 128), _t(4, 2, 16, 128).to(e4m3)
+    scales = dict(k_scale=_t(2, dtype=f32), v_scale=_t(2, dtype=f32))
+    return [
+        (cp.rms_norm, dict(x=_t(4, 64), weight=_t(64), residual=_t(4, 64), out=_t(4, 64), residual_out=_t(4, 64)), {}),
+        (cp.w4_matvec, dict(x=_t(2, 256), weight=_t(32, 128, dtype=torch.uint8), scale=_t(32, 2), out=_t(2, 32)), {}),
+        (cp.w4_matvec, dict(x=_t(2, 256).to(e4m3), weight=_t(32, 128, dtype=torch.uint8), scale=_t(32, 2), x_scale=_t(2, dtype=f32)), {}),
+        (cp.kv_append, dict(q=q, k=k, v=k.clone(), positions=_t(3, dtype=torch.int32), slots=_t(3, dtype=torch.int64),
+                            inv_freq=_t(64, dtype=f32), k_cache=cache, v_cache=cache.clone(), q_out=q.clone(), **scales), {}),
+        (cp.paged_attention, dict(q=q, k_cache=cache, v_cache=cache.clone(), table=_t(3, 2, dtype=torch.int32),
+                                  lengths=_t(3, dtype=torch.int32), out=q.clone(), lse=_t(3, 8, dtype=f32), **scales),
+         dict(max_length=32, return_lse=True))]
+
+
+@pytest.mark.parametrize("i", range(5))
+def test_no_gradient_is_cut_off(i):
+    """A tensor that requires a gradient is refused, unless none are asked for."""
+    f, tensors, rest = _calls()[i]
+    with pytest.raises(ValueError, match="GPU"):
+        f(**tensors, **rest)
+    for name, t in tensors.items():
+        if not t.is_floating_point():
+            continue
+        wants = t.detach().clone().requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            f(**{**tensors, name: wants}, **rest)
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            f(**{**tensors, name: wants}, **rest)
