@@ -25,6 +25,7 @@ using at::Tensor;
 
 PyObject* g_error = nullptr;        // CoverPruneError
 PyObject* g_raw_stream = nullptr;   // device index -> current stream's handle
+PyObject* g_device = nullptr;       // -> current device's index
 
 constexpr ScalarType kE4m3 = ScalarType::Float8_e4m3fn;
 
@@ -124,10 +125,17 @@ bool truth(PyObject* o) {
   return v != 0;
 }
 
-// The current stream of a tensor's GPU.  Everything is checked by then, so a
-// host pointer never reaches a kernel.
+// The current stream of the tensors' GPU, which has to be the current one: that is
+// where the library launches.  Everything is checked by then, so a host pointer
+// never reaches a kernel.
 void* stream_of(at::Device dev) {
   if (!dev.is_cuda()) raise(PyExc_ValueError, "tensors must be on the GPU, got %s", dev.str().c_str());
+  PyObject* current = PyObject_CallNoArgs(g_device);
+  if (!current) throw Raised();
+  const long now = PyLong_AsLong(current);
+  Py_DECREF(current);
+  if (now == -1 && PyErr_Occurred()) throw Raised();
+  if (now != dev.index()) raise(PyExc_ValueError, "tensors must be on the current GPU, %ld, got %s", now, dev.str().c_str());
   PyObject* index = PyLong_FromLong(dev.index());
   if (!index) throw Raised();
   PyObject* s = PyObject_CallOneArg(g_raw_stream, index);
@@ -331,18 +339,19 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// CoverPruneError and the function that gives a device's current stream.
+// CoverPruneError and the functions that give a device's current stream and the
+// current device.
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 2) {
-    PyErr_SetString(PyExc_TypeError, "init(error, raw_stream)");
+  if (n != 3) {
+    PyErr_SetString(PyExc_TypeError, "init(error, raw_stream, device)");
     return nullptr;
   }
-  Py_INCREF(args[0]);
-  Py_INCREF(args[1]);
-  Py_XDECREF(g_error);
-  Py_XDECREF(g_raw_stream);
-  g_error = args[0];
-  g_raw_stream = args[1];
+  PyObject** const kept[] = {&g_error, &g_raw_stream, &g_device};
+  for (int i = 0; i < 3; ++i) {
+    Py_INCREF(args[i]);
+    Py_XDECREF(*kept[i]);
+    *kept[i] = args[i];
+  }
   Py_RETURN_NONE;
 }
 

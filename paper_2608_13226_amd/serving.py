@@ -33,7 +33,7 @@ class _Unloaded:
             raise CoverPruneError(f"{os.path.join(HERE, '_serving.so')} is missing: build it with "
                                   f"`python -m paper_2608_13226_amd.build`")
         from . import _serving
-        _serving.init(CoverPruneError, _raw_stream)
+        _serving.init(CoverPruneError, _raw_stream, _device)
         _native = _serving
         return getattr(_serving, name)
 
@@ -42,9 +42,10 @@ def _any_raw_stream(index: int) -> int:
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# torch's own function for the handle of a device's current stream, where it
-# has one: a fifth of the time of making a Stream object.
+# torch's own functions for the handle of a device's current stream and for the
+# current device, where it has them: a fifth of the time of making a Stream object.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _any_raw_stream)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _native = _Unloaded()
 
 

@@ -75,3 +75,24 @@ def test_in_a_graph(length):
         want = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {i}"
+
+
+def test_tensors_of_another_gpu_than_the_current_one():
+    """Refused by each operator: the library launches on the current GPU.  (One GPU is enough: the binding is told
+    that another is current.)"""
+    import paper_2608_13226_amd as cp
+    from paper_2608_13226_amd import serving
+    step = _Step()
+    want = [t.clone() for t in step()]
+    q = torch.zeros(3, 8, 128, device="cuda", dtype=BF)
+    calls = [lambda: cp.rms_norm(step.x, step.gain), lambda: cp.w4_matvec(step.x, *step.wo),
+             lambda: cp.kv_append(q, q[:, :2], q[:, :2], step.positions, step.slots, step.inv, step.k, step.v),
+             lambda: cp.paged_attention(q, step.k, step.v, step.table, step.lengths)]
+    serving._native.init(cp.CoverPruneError, serving._raw_stream, lambda: torch.cuda.current_device() + 1)
+    try:
+        for call in calls:
+            with pytest.raises(ValueError, match="current GPU"):
+                call()
+    finally:
+        serving._native.init(cp.CoverPruneError, serving._raw_stream, serving._device)
+    assert all(torch.equal(a, b) for a, b in zip(step(), want))
