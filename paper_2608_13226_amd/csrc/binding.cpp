@@ -98,6 +98,12 @@ Tensor output(PyObject* o, const char* name, ScalarType type, at::IntArrayRef sh
   return t;
 }
 
+// The call has written t (where it is defined): autograd then knows that what it
+// has kept of t is gone.
+void written(const Tensor& t) {
+  if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 template <class T>
 T* at_of(const Tensor& t) { return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr; }
 
@@ -174,6 +180,7 @@ PyObject* rms_norm(PyObject* const* a) {
   const Tensor ro = r.defined() ? output(a[7], "residual_out", t, {rows, d}, dev) : Tensor();
   check(coverprune_rms_norm(x.data_ptr(), code(t), rows, d, at_of<void>(r), w.data_ptr(), float(eps), out.data_ptr(), code(ot),
                             at_of<float>(scale), at_of<void>(ro), stream_of(dev)));
+  written(out), written(scale), written(ro);
   PyObject* o = PyTuple_New(3);
   if (!o) throw Raised();
   PyTuple_SET_ITEM(o, 0, wrap(out));
@@ -211,6 +218,7 @@ PyObject* w4_matvec(PyObject* const* a) {
   const Tensor y = output(a[6], "out", yt, {m, n}, dev);
   check(coverprune_w4_matvec(x.data_ptr(), code(xt), at_of<float>(xs), at_of<uint8_t>(w), s.data_ptr(), at_of<uint8_t>(z), m, n, k,
                              k / groups, code(t), y.data_ptr(), code(yt), stream_of(dev)));
+  written(y);
   return wrap(y);
 }
 
@@ -278,6 +286,7 @@ PyObject* kv_append(PyObject* const* a) {
                              at_of<int32_t>(pos), at_of<int64_t>(slots), at_of<float>(inv), 2 * half, inter, float(magnitude),
                              at_of<void>(qo), kc.data_ptr(), vc.data_ptr(), code(c.type), c.pages, c.page, at_of<float>(ks),
                              at_of<float>(vs), stream_of(dev)));
+  written(qo), written(kc), written(vc);
   return wrap(qo);
 }
 
@@ -315,6 +324,7 @@ PyObject* paged_attention(PyObject* const* a) {
                                    c.page, at_of<float>(ks), at_of<float>(vs), at_of<int32_t>(table), width,
                                    at_of<int32_t>(lengths), longest, window, scale, out.data_ptr(), at_of<float>(lse),
                                    at_of<void>(ws), ws.defined() ? ws.nbytes() : 0, stream));
+  written(out), written(lse), written(ws);
   if (!return_lse) return wrap(out);
   PyObject* o = PyTuple_New(2);
   if (!o) throw Raised();

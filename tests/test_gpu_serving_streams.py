@@ -96,3 +96,33 @@ def test_tensors_of_another_gpu_than_the_current_one():
     finally:
         serving._native.init(cp.CoverPruneError, serving._raw_stream, serving._device)
     assert all(torch.equal(a, b) for a, b in zip(step(), want))
+
+
+def test_autograd_knows_what_was_written():
+    """A tensor that an operator writes counts as modified in place, so that a backward pass through its old values raises."""
+    import paper_2608_13226_amd as cp
+    step = _Step()
+    q = torch.zeros(3, 8, 128, device="cuda", dtype=BF)
+    k = torch.zeros(3, 2, 128, device="cuda", dtype=BF)
+    out, y, lse = torch.empty_like(step.x), torch.empty_like(step.x), torch.empty(3, 8, device="cuda")
+    codes = torch.empty(step.x.shape, device="cuda", dtype=torch.float8_e4m3fn)
+    scale, r = torch.empty(3, device="cuda"), step.h.clone()
+    o, q2 = torch.empty_like(q), torch.empty_like(q)
+    ws = torch.empty(1 << 22, device="cuda", dtype=torch.uint8)
+    calls = [(lambda: cp.rms_norm(step.x, step.gain, residual=r, residual_out=r, out=out), [out, r]),
+             (lambda: cp.rms_norm(step.x, step.gain, quantize=True, out=codes, out_scale=scale), [codes, scale]),
+             (lambda: cp.w4_matvec(step.x, *step.wo, out=y), [y]),
+             (lambda: cp.kv_append(q, k, k, step.positions, step.slots, step.inv, step.k, step.v, q_out=q2), [step.k, step.v, q2]),
+             (lambda: cp.paged_attention(q, step.k, step.v, step.table, step.lengths, out=o, lse=lse, workspace=ws), [o, lse, ws])]
+    for call, outputs in calls:
+        before = [t._version for t in outputs]
+        call()
+        assert all(t._version > v for t, v in zip(outputs, before))
+    w = torch.ones_like(step.k, requires_grad=True)
+    loss = (w * step.k).float().sum()
+    cp.kv_append(q, k, k, step.positions, step.slots, step.inv, step.k, step.v)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    with torch.inference_mode():
+        cache = torch.zeros_like(step.k)
+        cp.kv_append(None, k, k, step.positions, step.slots, step.inv, cache, torch.zeros_like(cache))
