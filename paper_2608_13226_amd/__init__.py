@@ -110,6 +110,20 @@ def library() -> ctypes.CDLL:
     if not os.path.exists(path):
         raise CoverPruneError(f"{path} is missing: build it with `python -m paper_2608_13226_amd.build`")
     lib = ctypes.CDLL(path)
+    try:
+        version = lib.coverprune_abi_version()
+        if version != ABI_VERSION:
+            raise CoverPruneError(f"{path} has ABI {version}, this binding needs {ABI_VERSION}: rebuild it")
+        _declare(lib)
+    except AttributeError as e:
+        # A library built before an entry point was added; its ABI has not changed otherwise.
+        raise CoverPruneError(f"{path} is older than this binding ({e}): rebuild it") from None
+    _lib = lib
+    return lib
+
+
+def _declare(lib: ctypes.CDLL) -> None:
+    """Argument and result types of every entry point."""
     i64, sz, vp, u32 = ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_uint32
     st = ctypes.c_int
     lib.coverprune_fst_cost_workspace.argtypes = [i64, i64, ctypes.c_int]
@@ -178,11 +192,6 @@ def library() -> ctypes.CDLL:
     lib.coverprune_paged_attention.restype = st
     lib.coverprune_uncovered_cost.argtypes = [_Weights]
     lib.coverprune_uncovered_cost.restype = ctypes.c_float
-    if lib.coverprune_abi_version() != ABI_VERSION:
-        raise CoverPruneError(f"{path} has ABI {lib.coverprune_abi_version()}, this binding needs {ABI_VERSION}: "
-                              f"rebuild it")
-    _lib = lib
-    return lib
 
 
 def _check(status: int) -> None:

@@ -222,3 +222,17 @@ def test_no_gradient_is_cut_off(i):
             f(**{**tensors, name: wants}, **rest)
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
             f(**{**tensors, name: wants}, **rest)
+
+
+@pytest.mark.parametrize("version,match", [(2, "older than this binding.*rebuild"), (1, "ABI 1.*rebuild")])
+def test_a_library_built_before_these_operators(monkeypatch, tmp_path, version, match):
+    """One that lacks entry points is named as such, whatever is called first; another ABI is said to be one."""
+    import subprocess
+    import paper_2608_13226_amd as cp
+    src, lib = tmp_path / "old.c", tmp_path / f"libold{version}.so"
+    src.write_text(f"int coverprune_abi_version(void) {{ return {version}; }}\n")
+    subprocess.run(["gcc", "-shared", "-fPIC", str(src), "-o", str(lib)], check=True)
+    monkeypatch.setattr(cp, "_lib", None)
+    monkeypatch.setattr(cp, "library_path", lambda: str(lib))
+    with pytest.raises(cp.CoverPruneError, match=match):
+        cp.uncovered_cost((1.0, 1.0, 1.0))
