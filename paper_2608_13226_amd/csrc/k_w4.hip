@@ -102,17 +102,25 @@ __device__ __forceinline__ void lds_barrier() {
 // One y (without x's scale) as the formula says, code by code.  The kernels take
 // the zero points off the groups' sums, which is another thing where x is
 // infinite, or a sum past float32's range; such results are found again here.
+// NaN ends it with its group.  (64 x 3584 x 28672: 33 us, a row with an infinity
+// 0.12 ms, 64 of them 2.1, 64 rows of NaN 0.11.)
 template <class T>
 __device__ __forceinline__ float by_formula(const W4Params& p, int64_t m, int64_t n) {
   const int groups = p.k / p.group;
+  const uint16_t* x = static_cast<const uint16_t*>(p.x) + m * p.k;
+  const uint8_t* w = p.weight + n * (p.k / 2);
   float y = 0.f;
   for (int i = 0; i < groups && y == y; ++i) {
     const float zero = p.zero ? float(p.zero[n * groups + i]) : 8.f;
     float sum = 0.f;
-    for (int j = i * p.group; j < (i + 1) * p.group; j += 2) {
-      const int two = p.weight[n * (p.k / 2) + j / 2];
-      sum = fmaf(load1<T>(p.x, m * p.k + j), float(two & 15) - zero, sum);
-      sum = fmaf(load1<T>(p.x, m * p.k + j + 1), float(two >> 4) - zero, sum);
+    // (One load of x at a time: the kernels' registers are for their own loop.)
+#pragma unroll 1
+    for (int j = i * p.group; j < (i + 1) * p.group; j += 8) {
+      const uint32_t eight = *reinterpret_cast<const uint32_t*>(w + j / 2);
+      float v[8];
+      load8<T>(x, j, v);
+#pragma unroll
+      for (int l = 0; l < 8; ++l) sum = fmaf(v[l], float(eight >> 4 * l & 15) - zero, sum);
     }
     y = fmaf(sum, load1<T>(p.scale, n * groups + i), y);
   }
