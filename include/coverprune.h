@@ -508,8 +508,8 @@ cp_status coverprune_lite_select(const void* feats, cp_dtype dtype, int64_t n, i
 /* Root-mean-square norm.
  *   h = x + residual (float32),  y_j = h_j weight_j / sqrt(mean_j h_j^2 + eps)
  *
- *   x         [rows, d], dtype CP_BF16, CP_F16 or CP_F32; 1 <= d <= 65536 (the
- *             rows are read 16 bytes at a time when d % 8 == 0)
+ *   x         [rows, d], dtype CP_BF16, CP_F16 or CP_F32; rows < 2^31,
+ *             1 <= d <= 65536
  *   residual  [rows, d] dtype, or NULL: h = x
  *   weight    [d] dtype
  *   eps       finite, >= 0
@@ -535,8 +535,10 @@ cp_status coverprune_rms_norm(const void* x, cp_dtype dtype, int64_t rows, int64
  *   group    a multiple of 32 that divides k (k <= 2^20)
  *   dtype    CP_BF16 or CP_F16
  *   y        [m, n], y_dtype == dtype or CP_F32
- * The time is that of reading the weights up to m = 16; every further 16 to 64 rows
- * read them again (from a cache, where they fit one).
+ * Infinite and NaN x give what the formula gives, at the cost of finding the
+ * results that are not finite code by code.  Up to m = 16 the weights are read
+ * once; every further 16 to 64 rows read them again (from a cache, where they fit
+ * one).
  */
 cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_scale, const uint8_t* weight,
                                const void* scale, const uint8_t* zero, int64_t m, int64_t n, int64_t k, int64_t group,
@@ -552,7 +554,8 @@ cp_status coverprune_w4_matvec(const void* x, cp_dtype x_dtype, const float* x_s
  *   q, k, v    [tokens, hq or hk, d], dtype CP_BF16 or CP_F16; a token's heads
  *              are contiguous, tokens are *_stride elements apart, so that
  *              the three can be views of one projection's output.  q may be NULL.
- *              Rows that are not 16-byte aligned are read element by element.
+ *              Elements go eight at a time where d, rot and the rows' alignment
+ *              (16 bytes) allow, four where half of that, else one by one.
  *   positions  [tokens] int32: kept tokens have the positions they had before
  *              the prune, so there may be gaps
  *   slots      [tokens] int64: page * page_size + offset, where each token's key
@@ -589,7 +592,9 @@ cp_status coverprune_kv_append(const void* q, int64_t q_stride, const void* k, i
  *   max_length  the longest length, known to the host; 1 <= max_length <= width * page_size
  *   window      > 0: only the last `window` tokens count; 0: all
  *   scale       finite; 1 / sqrt(d) is the usual choice
- *   out         [batch, hq, d] dtype
+ *   out         [batch, hq, d] dtype.  The softmax's weights are float32; with CP_F16
+ *               they meet the values with 22 bits, and those below 2^-36 of the
+ *               largest as 0
  *   lse         [batch, hq] float (may be NULL): log sum_j exp(scale q . k_j)
  *   workspace   coverprune_paged_attention_workspace bytes (0 for bad sizes and
  *               where none is needed): partial results of sequences cut into runs

@@ -6,7 +6,7 @@
 // copied.  Bound by memory: every element is read and written once.  A block
 // works on one token, or on several that have few heads: a token's R/2 angles
 // go to LDS once and serve all its heads.  6271 tokens of 32 + 32 heads of 64 in
-// 32.5 us (4.7 TB/s), 1638 of 28 + 4 heads of 128 to e4m3 in 8.3 us.
+// 31.7 us (4.85 TB/s), 1638 of 28 + 4 heads of 128 to e4m3 in 7.7 us.
 //
 // The angle is reduced to a fraction of a turn in float64 (32 bits of
 // position and 24 of frequency do not fit a float32 product, whose error

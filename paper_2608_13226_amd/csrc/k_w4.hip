@@ -214,8 +214,8 @@ __device__ __forceinline__ void spread(u32x4 v, u32x4* x) {
 // / SHARE rows, SHARE neighbouring lanes hold one row: each loads its share of
 // the row's x once and they pass it on; row r of x is then the product's rows
 // SHARE r to SHARE r + SHARE - 1, all alike.  At 1 x 3584 x 28672, groups of
-// 128, 15.0 us (3.5 TB/s) over weights that pass the caches, 11.8 where they
-// stay; at 16 rows 17.6 (3.0 TB/s) and 14.9.
+// 128, 14.5 us (3.6 TB/s) over weights that pass the caches, 12.1 where they
+// stay; at 16 rows 17.9 (3.0 TB/s) and 15.9.
 template <class T, bool X8, int SPAN, int RT, int SHARE>
 __global__ __launch_bounds__(SHARE == 4 ? 1024 : 512) void w4_few_kernel(W4Params p, int64_t first_block) {
   constexpr int kGroups = 4 / SPAN;
@@ -382,12 +382,13 @@ __device__ __forceinline__ float add2<F16>(uint32_t w, float c) {
 // sums beside them, while it works on the 256 before.  Waves: 8 by outputs (16
 // each) times 2 by k; codes are loaded two turns ahead.
 //
-// Bound by instruction issue: at 64 x 3584 x 28672, groups of 64, 32 us (1.9
-// TB/s of codes, 410 TFLOP/s); of a SIMD's cycles 54 % issue vector
-// instructions (141 a wave and turn, 28 of them to widen the codes) and the
-// matrix cores work in 31 %.  32 outputs a wave read LDS half as often but do not
-// fit the registers of 16 waves (44 us; 40 with 8 waves), turns of 512 k change
-// nothing (34).
+// At 64 x 3584 x 28672, groups of 64, 32 us (1.9 TB/s of codes, 410 TFLOP/s).
+// Nothing is full: of a SIMD's cycles 55 % issue vector instructions (153 a wave
+// and turn, 28 of them to widen the codes, beside 20 matrix ones), the matrix
+// cores work in 30 %, LDS in 32 %; the waves wait in 44 % of theirs, at the turn's
+// barrier among others, with no second block on the compute unit.  32 outputs a
+// wave read LDS half as often but do not fit the registers of 16 waves (44 us; 40
+// with 8 waves), turns of 512 k change nothing (34).
 constexpr int kWideRows = 128;
 constexpr int kWideGroups = 64;                   // whose scales are in LDS at a time
 template <class T, bool X8, int SPAN, int MT>
@@ -569,29 +570,31 @@ hipError_t launch_few(const W4Params& p, hipStream_t stream) {
   });
 }
 
-// Which kernel (rows x k x outputs, groups of 128, bf16; us of one call in a
-// graph, over weights that together pass the caches; a tile is 16 rows by 16
-// outputs):
+// Which kernel (rows x k x outputs, groups of 128, bf16, over weights that
+// together pass the caches; us of one call in a graph, both sides of each rule
+// from one sweep; a tile is 16 rows by 16 outputs):
 //   - more than 16 rows and many outputs: the wide one, whose time hardly
 //     depends on either up to a block a compute unit, while that of the other
 //     grows with rows x outputs.  With 32 rows a block they meet near 655360
-//     (32x3584x28672 22.2 against 28.0, 64x3584x12288 20.6 against 21.8,
-//     64x1792x16384 13.2 against 16.8; but 32x3584x18000 21.5 against 20.9,
-//     48x3584x12288 20.2 against 18.3), while its blocks are not more than
-//     compute units; with 64 near 2^20 (64x3584x28672 33.0 against 46.6; but
-//     48x3584x18000 32.0 against 27.2);
-//   - up to 4 rows, lanes share x four ways (1x3584x4608 5.1 against 5.5 two ways
-//     and 6.0 with none, 1x14336x3584 9.2, 14.0 and 15.0); up to 8 rows, two ways
-//     (8x2048x12000 5.9 against 6.5 with none).  Shared four ways, more outputs
-//     a wave gain nothing (1x3584x28672 15.0 and 14.9);
+//     (32x3584x28672 23.5 against 28.7, 64x3584x12288 21.2 against 22.6,
+//     64x1792x16384 13.8 against 18.0; but 32x3584x18000 21.4 against 20.5,
+//     48x3584x12288 21.0 against 19.7), while its blocks are not more than
+//     compute units; with 64 near 2^20 (64x3584x28672 31.3 against 46.2; but
+//     48x3584x18000 29.9 against 26.7);
+//   - up to 4 rows, lanes share x four ways (1x3584x4608 5.6 against 6.3 two ways
+//     and 7.1 with none, 1x14336x3584 9.1, 13.9 and 15.1, 1x3584x28672 14.4, 16.0
+//     and 21.5); up to 8 rows, two ways (8x3584x28672 16.3 against 17.5 with none,
+//     8x2048x12000 6.8 and 7.5);
 //   - 16 outputs a wave while there are fewer tiles than compute units
-//     (16x14336x3584 15.4, with 32 19.0); then 32 (16x3584x4608 6.2, with 16 7.1,
-//     with 64 10.5; 24x3584x4608 8.6, with 64 10.6; 48x14336x3584 26.6, with 64
-//     30.9); and 64 above three blocks of 32 a compute unit (16x3584x28672 17.5,
-//     with 32 19.1; 64x2048x12000 14.8 and 15.7; but 48x2048x12000 14.0 and 13.1);
-//   - 8 waves a block, 16 for a long k (one row, n = 3584, k = 14336: 8.4 against
-//     9.5; but n = 28672, k = 3584 14.1 against 12.1), 4 where each holds 64
-//     outputs.
+//     (16x14336x3584 15.5, with 32 19.5); then 32 (16x3584x4608 7.1, with 16 8.4,
+//     with 64 11.4; 24x3584x4608 8.8, with 64 11.3; 48x14336x3584 27.0, with 64
+//     32.1); and 64 from 1536 tiles on (16x3584x28672 17.9, with 32 19.5;
+//     64x2048x12000 15.8 and 16.0).  That bound is right for 16 rows only: with 17
+//     to 48 rows 32 outputs would be the faster up to some 3000 tiles
+//     (48x3584x12288 19.7, with 64 21.7, groups of 64 22.4 and 24.6, of 32 25.1 and
+//     27.6; 32x3584x18000 20.5 and 22.7; 48x2048x12000 13.7 and 15.1);
+//   - 8 waves a block, 16 for a long k (1x14336x3584 9.2 against 12.7 with 8; but
+//     1x3584x28672 19.9 against 14.4), 4 where each holds 64 outputs.
 template <class T, bool X8, int SPAN>
 hipError_t launch_span(const W4Params& p, hipStream_t stream) {
   const int64_t work = (p.m + 15) / 16 * 16 * p.n;
