@@ -28,7 +28,16 @@
  *   coverprune_w4_matvec   a few rows times 4-bit weights with group scales;
  *   coverprune_kv_append   position rotation, and keys and values into a paged
  *                          cache at the positions the tokens had in the video;
- *   coverprune_paged_attention  one new token of each sequence over that cache.
+ *   coverprune_paged_attention  one new token of each sequence over that cache;
+ *
+ * and, so that a session's cache stays small,
+ *
+ *   coverprune_kv_append4  the append to a cache of 4 bits, and
+ *   coverprune_paged_attention4  the attention over it;
+ *   coverprune_kv_gather   cached keys and values as dense rows again;
+ *   coverprune_paged_attention_mass  attention that adds up the weight each
+ *                          cached token gets, and
+ *   coverprune_kv_evict    the removal of those that got least.
  *
  * Conventions shared by every entry point
  *   - Token j has a feature row f_j (D values), a 3D position x_j (metres) and
@@ -82,9 +91,10 @@ typedef enum {
   CP_ERR_HIP = 4          /* the HIP runtime reported an error while enqueuing */
 } cp_status;
 
-/* CP_F16 and CP_E4M3 (8 bits: 3 after the leading one, exponents down to -6,
- * largest 448, no infinity) are types of the serving operators. */
-typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_F16 = 2, CP_E4M3 = 3 } cp_dtype;
+/* CP_F16, CP_E4M3 (8 bits: 3 after the leading one, exponents down to -6,
+ * largest 448, no infinity) and CP_E2M1 (4 bits, of caches: see
+ * coverprune_kv_append4) are types of the serving operators. */
+typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_F16 = 2, CP_E4M3 = 3, CP_E2M1 = 4 } cp_dtype;
 
 /* Weights of Eq. 8.  lambda_* >= 0 weight the feature, spatial and temporal
  * terms; kappa >= 0 shapes phi_kappa(z) = log(1 + kappa z) / log(1 + kappa),
@@ -607,6 +617,118 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
                                      const int32_t* table, int64_t width, const int32_t* lengths, int64_t max_length,
                                      int64_t window, float scale, void* out, float* lse, void* workspace,
                                      size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Serving operators that keep a session's cache small. */
+
+/* Position rotation, and keys and values into a paged cache of 4 bits.  The
+ * rotation is coverprune_kv_append's.  Each 32 consecutive elements x of a
+ * token's head are held as a power of two s and 32 codes:
+ *   s     the smallest power with max |x| <= 6 s, of 2^-125 .. 2^125 with
+ *         CP_BF16 and 2^-23 .. 2^13 with CP_F16 (so that every value that is held
+ *         is a normal or zero, finite one of dtype; in CP_F16 down to its
+ *         smallest), as a byte: its exponent plus 127
+ *   code  of x / s, at most 6 in size, rounded to nearest, ties to the even code:
+ *         0, 1/2, 1, 3/2, 2, 3, 4, 6 are codes 0 to 7, with a sign 8 to 15
+ * Keys are rotated in float64 for it, so that codes are those of the formula, up
+ * to float64's own rounding.  An infinity or NaN among the 32 makes them all
+ * NaN: the byte is 255 (and the codes 0).
+ *
+ *   q, k, v, dtype, positions, slots, inv_freq, rot, interleaved, magnitude, q_out
+ *              as for coverprune_kv_append, but q_out is not q; d a multiple of 32,
+ *              at most 4096.  Elements go eight at a time where q, k, v and their
+ *              strides are 16-byte aligned.
+ *   k_cache, v_cache  [pages, hk, page_size, d / 2] bytes: two codes each, the
+ *              even element's in the low half
+ *   k_scale, v_scale  [pages, hk, page_size, d / 32] bytes: the exponents
+ */
+cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
+                                const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
+                                int32_t interleaved, float magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
+                                int64_t pages, int64_t page_size, uint8_t* k_scale, uint8_t* v_scale, void* stream);
+
+/* Keys and values of some slots of a paged cache as dense rows.
+ *
+ *   k_cache, v_cache  [pages, hk, page_size, d]; cache_dtype == dtype, CP_E4M3 or
+ *              CP_E2M1 (d / 2 bytes a row then, d a multiple of 32)
+ *   k_scale, v_scale  CP_E4M3: [hk] float (NULL: 1); CP_E2M1: [pages, hk, page_size,
+ *              d / 32] exponent bytes; otherwise NULL
+ *   slots      [tokens] int64: page * page_size + offset; a negative slot, or one
+ *              past the last page, gives zeros.  A slot may be given twice.
+ *   k_out, v_out  [tokens, hk, d], dtype CP_BF16 or CP_F16: the cache's elements, or
+ *              what they stand for rounded to dtype
+ */
+cp_status coverprune_kv_gather(const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages, int64_t page_size,
+                               int64_t hk, int64_t d, const void* k_scale, const void* v_scale, const int64_t* slots,
+                               int64_t tokens, void* k_out, void* v_out, cp_dtype dtype, void* stream);
+
+/* coverprune_paged_attention over a cache of 4 bits.
+ *
+ *   k_cache, v_cache, k_scale, v_scale  as coverprune_kv_append4 writes them; what they
+ *              stand for is taken to dtype (exactly, where dtype has been theirs from the
+ *              start).  Values that are NaN count where their token's weight is 0, too.
+ *   the rest   as for coverprune_paged_attention, the workspace too
+ */
+cp_status coverprune_paged_attention4(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                      const uint8_t* k_cache, const uint8_t* v_cache, int64_t pages, int64_t page_size,
+                                      const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* table, int64_t width,
+                                      const int32_t* lengths, int64_t max_length, int64_t window, float scale, void* out,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* coverprune_paged_attention or coverprune_paged_attention4 that also adds up the weight
+ * that each cached token gets:
+ *   mass[b, h, j] += sum over the query heads i that read key-value head h of
+ *                    softmax_j(scale q_i . k_j)
+ * over the sequence's tokens j (with a window, the last `window`); other masses
+ * stay as they are.  A head without a score above -inf adds nothing, one with a NaN
+ * among its scores adds NaN to all.  Out and lse are those of the other calls.
+ *
+ *   cache_dtype  dtype, CP_E4M3 or CP_E2M1; k_scale and v_scale go with it as for
+ *              coverprune_kv_gather
+ *   mass       [batch, hk, mass_span] float, mass_span >= max_length
+ *   workspace  coverprune_paged_attention_mass_workspace bytes, 4 * batch * hq *
+ *              max_length of them for the scores
+ */
+size_t coverprune_paged_attention_mass_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
+                                                 int64_t window);
+cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                          const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages,
+                                          int64_t page_size, const void* k_scale, const void* v_scale,
+                                          const int32_t* table, int64_t width, const int32_t* lengths, int64_t max_length,
+                                          int64_t window, float scale, float* mass, int64_t mass_span, void* out, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* The tokens of least mass leave the cache, of each sequence and key-value head
+ * its own: of n > keep tokens the first `sink`, the last `recent` and, of the
+ * others, those of largest mass stay (NaN below all others, -0 as 0; of equal
+ * ones the earlier), `keep` in all.  They close the gaps in place: with f = keep -
+ * recent, those below f do not move, those from f to n - recent move to the
+ * places below f that fall vacant, in order, and the last `recent` go to f and on,
+ * in order.  Attention does not go by the order, but `window` does.  Slots from
+ * keep on are left as they were.
+ *
+ *   k_cache, v_cache  [pages, hk, page_size, d], cache_dtype CP_BF16, CP_F16, CP_E4M3 or
+ *              CP_E2M1; d a multiple of 8 (CP_E2M1: of 32), at most 4096;
+ *              pages * hk * page_size < 2^32
+ *   k_scale, v_scale  CP_E2M1: the exponents, which move with their rows; otherwise NULL
+ *   table, lengths, max_length  as for coverprune_paged_attention.  Pages that two
+ *              sequences share are the caller's error.
+ *   mass       [batch, hk, mass_span] float, mass_span >= max_length
+ *   keep       1 <= keep < 2^31; recent >= 0, sink >= 0, recent + sink <= keep
+ *   kept       [batch, hk, keep] int32 output: which token is now at each place, -1
+ *              from the new length on
+ *   mass_out   [batch, hk, mass_span] float output, may be mass: the masses in the new
+ *              order, 0 from the new length on
+ *   lengths_out  [batch] int32 output, not lengths: the new lengths, at most keep
+ *   workspace  coverprune_kv_evict_workspace bytes
+ */
+size_t coverprune_kv_evict_workspace(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length);
+cp_status coverprune_kv_evict(void* k_cache, void* v_cache, cp_dtype cache_dtype, int64_t pages, int64_t page_size, int64_t hk,
+                              int64_t d, uint8_t* k_scale, uint8_t* v_scale, const int32_t* table, int64_t batch,
+                              int64_t width, const int32_t* lengths, int64_t max_length, const float* mass,
+                              int64_t mass_span, int64_t keep, int64_t recent, int64_t sink, int32_t* kept, float* mass_out,
+                              int32_t* lengths_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Measurement: the latency floor of one greedy step on this device (Sec. 3.5).

@@ -25,7 +25,8 @@ import torch
 
 __all__ = ["fst_cost", "fst_capacity", "prune", "sgs_select", "sgs_select_batch", "sgs_literal_select", "knn",
            "sgs_local_select", "lite_select", "uncovered_cost", "step_floor", "library", "library_path", "CoverPruneError",
-           "DEFAULT_KAPPA", "rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention"]
+           "DEFAULT_KAPPA", "rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention", "kv_append4",
+           "kv_gather", "paged_attention4", "paged_attention_mass", "kv_evict", "KvEvictResult"]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libcoverprune.so"
@@ -190,6 +191,24 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.coverprune_paged_attention.argtypes = [vp, dt, i64, i64, i64, i64, vp, vp, dt, i64, i64, vp, vp, vp, i64, vp, i64,
                                                i64, f32, vp, vp, vp, sz, vp]
     lib.coverprune_paged_attention.restype = st
+    lib.coverprune_kv_append4.argtypes = [vp, i64, vp, i64, vp, i64, dt, i64, i64, i64, i64, vp, vp, vp, i64, i32, f32, vp,
+                                          vp, vp, i64, i64, vp, vp, vp]
+    lib.coverprune_kv_append4.restype = st
+    lib.coverprune_kv_gather.argtypes = [vp, vp, dt, i64, i64, i64, i64, vp, vp, vp, i64, vp, vp, dt, vp]
+    lib.coverprune_kv_gather.restype = st
+    lib.coverprune_paged_attention4.argtypes = [vp, dt, i64, i64, i64, i64, vp, vp, i64, i64, vp, vp, vp, i64, vp, i64, i64,
+                                                f32, vp, vp, vp, sz, vp]
+    lib.coverprune_paged_attention4.restype = st
+    lib.coverprune_paged_attention_mass_workspace.argtypes = [i64, i64, i64, i64, i64, i64]
+    lib.coverprune_paged_attention_mass_workspace.restype = sz
+    lib.coverprune_paged_attention_mass.argtypes = [vp, dt, i64, i64, i64, i64, vp, vp, dt, i64, i64, vp, vp, vp, i64, vp, i64,
+                                                    i64, f32, vp, i64, vp, vp, vp, sz, vp]
+    lib.coverprune_paged_attention_mass.restype = st
+    lib.coverprune_kv_evict_workspace.argtypes = [i64, i64, i64, i64, i64]
+    lib.coverprune_kv_evict_workspace.restype = sz
+    lib.coverprune_kv_evict.argtypes = [vp, vp, dt, i64, i64, i64, i64, vp, vp, vp, i64, i64, vp, i64, vp, i64, i64, i64, i64,
+                                        vp, vp, vp, vp, sz, vp]
+    lib.coverprune_kv_evict.restype = st
     lib.coverprune_uncovered_cost.argtypes = [_Weights]
     lib.coverprune_uncovered_cost.restype = ctypes.c_float
 
@@ -591,4 +610,5 @@ def lite_select(feats: torch.Tensor, pos: torch.Tensor, frame: torch.Tensor, cap
 
 
 # The serving layer's operators use the helpers above.
-from .serving import RmsNormResult, kv_append, paged_attention, rms_norm, w4_matvec  # noqa: E402
+from .serving import (KvEvictResult, RmsNormResult, kv_append, kv_append4, kv_evict, kv_gather,  # noqa: E402
+                      paged_attention, paged_attention4, paged_attention_mass, rms_norm, w4_matvec)

@@ -622,6 +622,7 @@ static bool serve_type(cp_dtype t, cp::ServeType* out) {
     case CP_F16: *out = cp::ServeType::kF16; return true;
     case CP_F32: *out = cp::ServeType::kF32; return true;
     case CP_E4M3: *out = cp::ServeType::kE4m3; return true;
+    case CP_E2M1: *out = cp::ServeType::kE2m1; return true;
   }
   return false;
 }
@@ -772,7 +773,87 @@ static cp_status check_attend(int64_t batch, int64_t hq, int64_t hk, int64_t d, 
 size_t coverprune_paged_attention_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                             int64_t window) {
   if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
-  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window);
+  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, false);
+}
+
+size_t coverprune_paged_attention_mass_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
+                                                 int64_t window) {
+  if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
+  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, true);
+}
+
+// Pages, table and lengths of a call over a paged cache.
+static cp_status check_pages(int64_t pages, int64_t page_size, int64_t hk, int64_t width, int64_t max_length) {
+  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
+  if (pages < 1 || pages > ((int64_t(1) << 32) - 1) / (hk * page_size))
+    return fail(CP_ERR_UNSUPPORTED, "pages = %lld: pages * hk * page_size must be in [1, 2^32)", (long long)pages);
+  if (width < 1 || width > (int64_t(1) << 31) / page_size || max_length > width * page_size)
+    return fail(CP_ERR_INVALID_ARG, "max_length = %lld over the table's %lld pages of %lld", (long long)max_length,
+                (long long)width, (long long)page_size);
+  return CP_OK;
+}
+
+// What all forms of the cache's attention take; `mass` asks for the form that adds to it.
+static cp_status attend(bool mass, cp::AttendParams& p, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                        cp_dtype held, int64_t page_size, int64_t width, int64_t window, size_t workspace_bytes, void* stream) {
+  cp_status st = check_attend(batch, hq, hk, d, p.max_length, window);
+  if (st != CP_OK) return st;
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if ((st = check_pages(p.pages, page_size, hk, width, p.max_length)) != CP_OK) return st;
+  if (!std::isfinite(p.scale)) return fail(CP_ERR_INVALID_ARG, "scale must be finite");
+  if (mass && (p.mass_span < p.max_length || p.mass_span >= int64_t(1) << 31))
+    return fail(CP_ERR_INVALID_ARG, "mass_span = %lld outside [max_length, 2^31)", (long long)p.mass_span);
+  if (batch == 0) return ok();
+  if (!p.q || !p.k_cache || !p.v_cache || !p.table || !p.lengths || !p.out)
+    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, table, lengths and out must be non-NULL");
+  if (held == CP_E2M1 && (!p.k_exps || !p.v_exps)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale must be non-NULL with a 4-bit cache");
+  if (mass && !p.mass) return fail(CP_ERR_INVALID_ARG, "mass must be non-NULL");
+  if (!aligned16(p.q) || !aligned16(p.k_cache) || !aligned16(p.v_cache) || !aligned16(p.out) || (mass && !aligned16(p.mass)))
+    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, out and mass must be 16-byte aligned");
+  if ((st = check_workspace(p.workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, p.max_length, window, mass))) != CP_OK)
+    return st;
+  p.batch = int(batch);
+  p.hq = int(hq);
+  p.hk = int(hk);
+  p.d = int(d);
+  p.page = int(page_size);
+  p.width = int(width);
+  p.page_shift = 0;
+  while ((int64_t(1) << p.page_shift) < page_size) ++p.page_shift;
+  p.page_magic = unsigned(((int64_t(1) << (31 + p.page_shift)) + page_size - 1) / page_size);
+  p.window = int(std::min<int64_t>(window, p.max_length));
+  serve_type(dtype, &p.type);
+  serve_type(held, &p.held);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = held == CP_E2M1 ? (mass ? cp::launch_attend4_mass(p, s) : cp::launch_attend4(p, s))
+                                 : (mass ? cp::launch_attend_mass(p, s) : cp::launch_attend(p, s));
+  if (e != hipSuccess) return hip_fail(e, "paged attention");
+  return ok();
+}
+
+static cp::AttendParams attend_params(const void* q, const void* k_cache, const void* v_cache, cp_dtype held, const void* k_scale,
+                                      const void* v_scale, int64_t pages, const int32_t* table, const int32_t* lengths,
+                                      int64_t max_length, float scale, void* out, float* lse, void* workspace) {
+  cp::AttendParams p = {};
+  p.q = q;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  if (held == CP_E2M1) {
+    p.k_exps = static_cast<const uint8_t*>(k_scale);
+    p.v_exps = static_cast<const uint8_t*>(v_scale);
+  } else {
+    p.k_scale = static_cast<const float*>(k_scale);
+    p.v_scale = static_cast<const float*>(v_scale);
+  }
+  p.table = table;
+  p.lengths = lengths;
+  p.out = out;
+  p.lse = lse;
+  p.pages = pages;
+  p.max_length = max_length;
+  p.scale = scale;
+  p.workspace = workspace;
+  return p;
 }
 
 cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
@@ -783,53 +864,207 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
                                      size_t workspace_bytes, void* stream) {
   cp_status st = check_attend(batch, hq, hk, d, max_length, window);
   if (st != CP_OK) return st;
-  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
-  if (cache_dtype != dtype && cache_dtype != CP_E4M3)
+  if (half_type(dtype) && cache_dtype != dtype && cache_dtype != CP_E4M3)
     return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: dtype or e4m3", (int)cache_dtype);
   if (cache_dtype != CP_E4M3 && (k_scale || v_scale)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e4m3 cache");
-  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
-  if (pages < 1 || pages > ((int64_t(1) << 32) - 1) / (hk * page_size))
-    return fail(CP_ERR_UNSUPPORTED, "pages = %lld: pages * hk * page_size must be in [1, 2^32)", (long long)pages);
-  if (width < 1 || width > (int64_t(1) << 31) / page_size || max_length > width * page_size)
-    return fail(CP_ERR_INVALID_ARG, "max_length = %lld over the table's %lld pages of %lld", (long long)max_length,
-                (long long)width, (long long)page_size);
-  if (!std::isfinite(scale)) return fail(CP_ERR_INVALID_ARG, "scale must be finite");
-  if (batch == 0) return ok();
-  if (!q || !k_cache || !v_cache || !table || !lengths || !out)
-    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, table, lengths and out must be non-NULL");
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
-    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache and out must be 16-byte aligned");
-  if ((st = check_workspace(workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window))) != CP_OK)
-    return st;
+  cp::AttendParams p = attend_params(q, k_cache, v_cache, cache_dtype, k_scale, v_scale, pages, table, lengths, max_length, scale,
+                                     out, lse, workspace);
+  return attend(false, p, dtype, batch, hq, hk, d, cache_dtype, page_size, width, window, workspace_bytes, stream);
+}
 
-  cp::AttendParams p;
+cp_status coverprune_paged_attention4(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                      const uint8_t* k_cache, const uint8_t* v_cache, int64_t pages, int64_t page_size,
+                                      const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* table, int64_t width,
+                                      const int32_t* lengths, int64_t max_length, int64_t window, float scale, void* out,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  cp::AttendParams p = attend_params(q, k_cache, v_cache, CP_E2M1, k_scale, v_scale, pages, table, lengths, max_length, scale, out,
+                                     lse, workspace);
+  return attend(false, p, dtype, batch, hq, hk, d, CP_E2M1, page_size, width, window, workspace_bytes, stream);
+}
+
+cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,
+                                          const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages,
+                                          int64_t page_size, const void* k_scale, const void* v_scale,
+                                          const int32_t* table, int64_t width, const int32_t* lengths, int64_t max_length,
+                                          int64_t window, float scale, float* mass, int64_t mass_span, void* out, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+  cp_status st = check_attend(batch, hq, hk, d, max_length, window);
+  if (st != CP_OK) return st;
+  if (half_type(dtype) && cache_dtype != dtype && cache_dtype != CP_E4M3 && cache_dtype != CP_E2M1)
+    return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: dtype, e4m3 or e2m1", (int)cache_dtype);
+  if (half_type(cache_dtype) && (k_scale || v_scale))
+    return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e4m3 or e2m1 cache");
+  cp::AttendParams p = attend_params(q, k_cache, v_cache, cache_dtype, k_scale, v_scale, pages, table, lengths, max_length, scale,
+                                     out, lse, workspace);
+  p.mass = mass;
+  p.mass_span = mass_span;
+  return attend(true, p, dtype, batch, hq, hk, d, cache_dtype, page_size, width, window, workspace_bytes, stream);
+}
+
+cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
+                                const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
+                                int32_t interleaved, float magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
+                                int64_t pages, int64_t page_size, uint8_t* k_scale, uint8_t* v_scale, void* stream) {
+  if (tokens < 0 || tokens >= (int64_t(1) << 31))
+    return fail(CP_ERR_INVALID_ARG, "tokens = %lld outside [0, 2^31)", (long long)tokens);
+  if (hq < 0 || hq > 65536 || (q && hq < 1)) return fail(CP_ERR_INVALID_ARG, "hq = %lld outside [1, 65536]", (long long)hq);
+  if (hk < 1 || hk > 65536) return fail(CP_ERR_INVALID_ARG, "hk = %lld outside [1, 65536]", (long long)hk);
+  if (d < 32 || d > 4096 || d % 32 != 0) return fail(CP_ERR_UNSUPPORTED, "d = %lld must be a multiple of 32, at most 4096", (long long)d);
+  if (rot < 0 || rot > d || rot % 2 != 0) return fail(CP_ERR_INVALID_ARG, "rot = %lld must be even, in [0, d]", (long long)rot);
+  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
+  if (pages < 1 || pages > (int64_t(1) << 40)) return fail(CP_ERR_INVALID_ARG, "pages = %lld outside [1, 2^40]", (long long)pages);
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if (!std::isfinite(magnitude)) return fail(CP_ERR_INVALID_ARG, "magnitude must be finite");
+  if ((q && q_stride < hq * d) || k_stride < hk * d || v_stride < hk * d)
+    return fail(CP_ERR_INVALID_ARG, "a token stride is smaller than a token's heads");
+  if (tokens == 0) return ok();
+  if (!k || !v || !positions || !slots || !k_cache || !v_cache || !k_scale || !v_scale || (rot && !inv_freq) || (q && !q_out))
+    return fail(CP_ERR_INVALID_ARG,
+                "k, v, positions, slots, inv_freq, k_cache, v_cache, k_scale, v_scale and (with q) q_out must be non-NULL");
+  if (q && q == q_out) return fail(CP_ERR_INVALID_ARG, "q_out must not be q");
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_out))
+    return fail(CP_ERR_INVALID_ARG, "k_cache, v_cache and q_out must be 16-byte aligned");
+
+  cp::KvAppend4Params p;
   p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.positions = positions;
+  p.slots = slots;
+  p.inv_freq = inv_freq;
+  p.q_out = q_out;
   p.k_cache = k_cache;
   p.v_cache = v_cache;
-  p.table = table;
-  p.lengths = lengths;
   p.k_scale = k_scale;
   p.v_scale = v_scale;
-  p.out = out;
-  p.lse = lse;
+  p.tokens = tokens;
   p.pages = pages;
-  p.max_length = max_length;
-  p.batch = int(batch);
   p.hq = int(hq);
   p.hk = int(hk);
   p.d = int(d);
+  p.rot = int(rot);
+  p.page = int(page_size);
+  p.magnitude = magnitude;
+  p.interleaved = interleaved != 0;
+  serve_type(dtype, &p.type);
+  hipError_t e = cp::launch_kv_append4(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kv append to 4 bits");
+  return ok();
+}
+
+cp_status coverprune_kv_gather(const void* k_cache, const void* v_cache, cp_dtype cache_dtype, int64_t pages, int64_t page_size,
+                               int64_t hk, int64_t d, const void* k_scale, const void* v_scale, const int64_t* slots,
+                               int64_t tokens, void* k_out, void* v_out, cp_dtype dtype, void* stream) {
+  if (tokens < 0 || tokens >= (int64_t(1) << 31))
+    return fail(CP_ERR_INVALID_ARG, "tokens = %lld outside [0, 2^31)", (long long)tokens);
+  if (hk < 1 || hk > 65536) return fail(CP_ERR_INVALID_ARG, "hk = %lld outside [1, 65536]", (long long)hk);
+  if (d < 1 || d > 4096) return fail(CP_ERR_INVALID_ARG, "d = %lld outside [1, 4096]", (long long)d);
+  if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
+  if (pages < 1 || pages > (int64_t(1) << 40)) return fail(CP_ERR_INVALID_ARG, "pages = %lld outside [1, 2^40]", (long long)pages);
+  if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
+  if (cache_dtype != dtype && cache_dtype != CP_E4M3 && cache_dtype != CP_E2M1)
+    return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: dtype, e4m3 or e2m1", (int)cache_dtype);
+  if (cache_dtype == CP_E2M1 && d % 32 != 0) return fail(CP_ERR_UNSUPPORTED, "d = %lld must be a multiple of 32 with a 4-bit cache", (long long)d);
+  if (half_type(cache_dtype) && (k_scale || v_scale))
+    return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e4m3 or e2m1 cache");
+  if (tokens == 0) return ok();
+  if (!k_cache || !v_cache || !slots || !k_out || !v_out || (cache_dtype == CP_E2M1 && (!k_scale || !v_scale)))
+    return fail(CP_ERR_INVALID_ARG, "k_cache, v_cache, slots, k_out, v_out and (4 bits) k_scale and v_scale must be non-NULL");
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(k_out) || !aligned16(v_out))
+    return fail(CP_ERR_INVALID_ARG, "k_cache, v_cache, k_out and v_out must be 16-byte aligned");
+
+  cp::KvGatherParams p;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.slots = slots;
+  p.k_out = k_out;
+  p.v_out = v_out;
+  p.tokens = tokens;
+  p.pages = pages;
+  p.hk = int(hk);
+  p.d = int(d);
+  p.page = int(page_size);
+  serve_type(dtype, &p.type);
+  serve_type(cache_dtype, &p.held);
+  hipError_t e = cp::launch_kv_gather(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kv gather");
+  return ok();
+}
+
+static cp_status check_evict(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t sink, int64_t max_length) {
+  if (batch < 0 || batch > 65535) return fail(CP_ERR_INVALID_ARG, "batch = %lld outside [0, 65535]", (long long)batch);
+  if (hk < 1 || hk > 65535) return fail(CP_ERR_INVALID_ARG, "hk = %lld outside [1, 65535]", (long long)hk);
+  if (keep < 1 || keep >= int64_t(1) << 31) return fail(CP_ERR_INVALID_ARG, "keep = %lld outside [1, 2^31)", (long long)keep);
+  if (recent < 0 || sink < 0 || recent > keep || sink > keep - recent)
+    return fail(CP_ERR_INVALID_ARG, "recent = %lld and sink = %lld must be >= 0, together at most keep = %lld", (long long)recent,
+                (long long)sink, (long long)keep);
+  if (max_length < 1 || max_length >= (int64_t(1) << 31) - 2048)
+    return fail(CP_ERR_INVALID_ARG, "max_length = %lld outside [1, 2^31 - 2048)", (long long)max_length);
+  return CP_OK;
+}
+
+size_t coverprune_kv_evict_workspace(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length) {
+  if (check_evict(batch, hk, keep, recent, 0, max_length) != CP_OK || batch == 0) return 0;
+  return cp::evict_workspace_bytes(batch, hk, keep, recent, max_length);
+}
+
+cp_status coverprune_kv_evict(void* k_cache, void* v_cache, cp_dtype cache_dtype, int64_t pages, int64_t page_size, int64_t hk,
+                              int64_t d, uint8_t* k_scale, uint8_t* v_scale, const int32_t* table, int64_t batch,
+                              int64_t width, const int32_t* lengths, int64_t max_length, const float* mass,
+                              int64_t mass_span, int64_t keep, int64_t recent, int64_t sink, int32_t* kept, float* mass_out,
+                              int32_t* lengths_out, void* workspace, size_t workspace_bytes, void* stream) {
+  cp_status st = check_evict(batch, hk, keep, recent, sink, max_length);
+  if (st != CP_OK) return st;
+  if ((st = check_pages(pages, page_size, hk, width, max_length)) != CP_OK) return st;
+  if (mass_span < max_length || mass_span >= int64_t(1) << 31)
+    return fail(CP_ERR_INVALID_ARG, "mass_span = %lld outside [max_length, 2^31)", (long long)mass_span);
+  if (!half_type(cache_dtype) && cache_dtype != CP_E4M3 && cache_dtype != CP_E2M1)
+    return fail(CP_ERR_UNSUPPORTED, "cache_dtype %d: bf16, f16, e4m3 or e2m1", (int)cache_dtype);
+  const bool four = cache_dtype == CP_E2M1;
+  if (d < 8 || d > 4096 || d % (four ? 32 : 8) != 0)
+    return fail(CP_ERR_UNSUPPORTED, "d = %lld must be a multiple of %d, at most 4096", (long long)d, four ? 32 : 8);
+  if (!four && (k_scale || v_scale)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale go with an e2m1 cache");
+  if (batch == 0) return ok();
+  if (!k_cache || !v_cache || !table || !lengths || !mass || !kept || !mass_out || !lengths_out || (four && (!k_scale || !v_scale)))
+    return fail(CP_ERR_INVALID_ARG,
+                "k_cache, v_cache, table, lengths, mass, kept, mass_out, lengths_out and (4 bits) k_scale and v_scale must be non-NULL");
+  if (lengths_out == lengths) return fail(CP_ERR_INVALID_ARG, "lengths_out must not be lengths");
+  if (!aligned16(k_cache) || !aligned16(v_cache)) return fail(CP_ERR_INVALID_ARG, "k_cache and v_cache must be 16-byte aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, cp::evict_workspace_bytes(batch, hk, keep, recent, max_length))) != CP_OK)
+    return st;
+
+  cp::KvEvictParams p;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.k_exps = four ? k_scale : nullptr;
+  p.v_exps = four ? v_scale : nullptr;
+  p.table = table;
+  p.lengths = lengths;
+  p.mass = mass;
+  p.mass_out = mass_out;
+  p.kept = kept;
+  p.lengths_out = lengths_out;
+  p.span = mass_span;
+  p.pages = pages;
+  p.max_length = max_length;
+  p.keep = keep;
+  p.recent = recent;
+  p.sink = sink;
+  p.batch = int(batch);
+  p.hk = int(hk);
   p.page = int(page_size);
   p.width = int(width);
-  p.page_shift = 0;
-  while ((int64_t(1) << p.page_shift) < page_size) ++p.page_shift;
-  p.page_magic = unsigned(((int64_t(1) << (31 + p.page_shift)) + page_size - 1) / page_size);
-  p.window = int(std::min<int64_t>(window, max_length));
-  p.scale = scale;
-  p.cache8 = cache_dtype == CP_E4M3;
-  serve_type(dtype, &p.type);
+  p.row_bytes = int(four ? d / 2 : cache_dtype == CP_E4M3 ? d : 2 * d);
+  p.exp_bytes = int(four ? d / 32 : 0);
   p.workspace = workspace;
-  hipError_t e = cp::launch_attend(p, static_cast<hipStream_t>(stream));
-  if (e != hipSuccess) return hip_fail(e, "paged attention");
+  hipError_t e = cp::launch_kv_evict(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kv evict");
   return ok();
 }
 

@@ -210,7 +210,7 @@ hipError_t launch_blocks(int64_t blocks, int threads, F launch) {
   return hipSuccess;
 }
 
-enum class ServeType { kBf16, kF16, kF32, kE4m3 };
+enum class ServeType { kBf16, kF16, kF32, kE4m3, kE2m1 };
 
 struct RmsNormParams {
   const void* x;                  // [rows, d]
@@ -266,16 +266,57 @@ struct KvAppendParams {
 };
 hipError_t launch_kv_append(const KvAppendParams& p, hipStream_t stream);
 
+// The caches of 4 bits: codes two a byte, the even dim low, and exponents of blocks of 32 dims.
+struct KvAppend4Params {
+  const void* q;                  // [tokens, hq, d] at token stride q_stride, or nullptr
+  const void* k;                  // [tokens, hk, d] at k_stride
+  const void* v;                  // [tokens, hk, d] at v_stride
+  int64_t q_stride, k_stride, v_stride;   // elements
+  const int32_t* positions;       // [tokens]
+  const int64_t* slots;           // [tokens]
+  const float* inv_freq;          // [rot / 2]
+  void* q_out;                    // [tokens, hq, d], with q
+  uint8_t* k_cache;               // [pages, hk, page, d / 2]
+  uint8_t* v_cache;
+  uint8_t* k_scale;               // [pages, hk, page, d / 32]
+  uint8_t* v_scale;
+  int64_t tokens, pages;
+  int hq, hk, d, rot, page;       // d % 32 == 0
+  float magnitude;
+  bool interleaved;
+  ServeType type;
+};
+hipError_t launch_kv_append4(const KvAppend4Params& p, hipStream_t stream);
+
+struct KvGatherParams {
+  const void* k_cache;            // [pages, hk, page, d], or d / 2 bytes of codes
+  const void* v_cache;
+  const void* k_scale;            // e4m3: [hk] float or nullptr; e2m1: [pages, hk, page, d / 32] exponents
+  const void* v_scale;
+  const int64_t* slots;           // [tokens]
+  void* k_out;                    // [tokens, hk, d]
+  void* v_out;
+  int64_t tokens, pages;
+  int hk, d, page;
+  ServeType type;                 // of the outputs
+  ServeType held;                 // `type`, kE4m3 or kE2m1 (d % 32 == 0)
+};
+hipError_t launch_kv_gather(const KvGatherParams& p, hipStream_t stream);
+
 struct AttendParams {
   const void* q;                  // [batch, hq, d]
-  const void* k_cache;            // [pages, hk, page, d]
+  const void* k_cache;            // [pages, hk, page, d], or d / 2 bytes of codes
   const void* v_cache;
   const int32_t* table;           // [batch, width]
   const int32_t* lengths;         // [batch]
   const float* k_scale;           // [hk] or nullptr, e4m3 caches
   const float* v_scale;
+  const uint8_t* k_exps;          // [pages, hk, page, d / 32], e2m1 caches
+  const uint8_t* v_exps;
   void* out;                      // [batch, hq, d]
   float* lse;                     // [batch, hq] or nullptr
+  float* mass;                    // [batch, hk, mass_span], launch_attend_mass and launch_attend4_mass
+  int64_t mass_span;              // >= max_length
   int64_t pages;                  // pages * hk * page < 2^32
   int64_t max_length;             // 1 <= max_length <= width * page < 2^31
   int batch, hq, hk, d, page, width;
@@ -283,12 +324,35 @@ struct AttendParams {
                                   // shift = ceil(log2 page), magic = ceil(2^(31 + shift) / page)
   int window;                     // 0: none
   float scale;
-  bool cache8;
   ServeType type;
+  ServeType held;                 // `type`, kE4m3 or (launch_attend4, launch_attend4_mass) kE2m1
   void* workspace;
 };
 // 0 where one launch writes the result.
-size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window);
+size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass);
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
+hipError_t launch_attend4(const AttendParams& p, hipStream_t stream);
+hipError_t launch_attend_mass(const AttendParams& p, hipStream_t stream);
+hipError_t launch_attend4_mass(const AttendParams& p, hipStream_t stream);
+
+struct KvEvictParams {
+  void* k_cache;                  // [pages, hk, page] rows of row_bytes
+  void* v_cache;
+  uint8_t* k_exps;                // [pages, hk, page] rows of exp_bytes (e2m1), or nullptr
+  uint8_t* v_exps;
+  const int32_t* table;           // [batch, width]
+  const int32_t* lengths;         // [batch]
+  const float* mass;              // [batch, hk, span]
+  float* mass_out;                // [batch, hk, span], may be mass
+  int32_t* kept;                  // [batch, hk, keep]
+  int32_t* lengths_out;           // [batch], not lengths
+  int64_t span, pages, max_length;  // 1 <= max_length <= min(span, width * page) < 2^31
+  int64_t keep, recent, sink;     // 1 <= keep < 2^31, 0 <= sink + recent <= keep
+  int batch, hk, page, width;
+  int row_bytes, exp_bytes;       // row_bytes a multiple of 8; exp_bytes 0 without exponents
+  void* workspace;
+};
+size_t evict_workspace_bytes(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length);
+hipError_t launch_kv_evict(const KvEvictParams& p, hipStream_t stream);
 
 }  // namespace cp

@@ -1,5 +1,5 @@
 // Types and conversions shared by the serving kernels (norm, 4-bit products,
-// cache append, cache attention).  8-bit values are e4m3: 3 bits after the
+// the cache's append, attention, read-back and eviction).  8-bit values are e4m3: 3 bits after the
 // leading one, exponents down to -6, largest 448, no infinity.
 #pragma once
 
@@ -204,6 +204,37 @@ __device__ __forceinline__ uint32_t widen2<F16, false>(uint32_t w) {
 template <>
 __device__ __forceinline__ uint32_t widen2<F16, true>(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
+}
+
+// 4-bit values are e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign), two a byte, the even
+// element in the low half, times a power of two for each 32 elements, which is held as
+// its exponent plus 127; 255 makes a block NaN.
+constexpr int kBlock4 = 32;
+
+// The power of two that an exponent byte stands for, as the conversions take it (they read its exponent alone).
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Byte `byte` of four bytes of codes as a packed pair of T, times the power: exact
+// where T holds the result, else rounded to nearest even.
+template <class T>
+__device__ __forceinline__ uint32_t open2(uint32_t w, float power, int byte);
+template <>
+__device__ __forceinline__ uint32_t open2<Bf16>(uint32_t w, float power, int byte) {
+  switch (byte) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, 3));
+  }
+}
+template <>
+__device__ __forceinline__ uint32_t open2<F16>(uint32_t w, float power, int byte) {
+  switch (byte) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, 3));
+  }
 }
 
 }  // namespace cp

@@ -1,12 +1,14 @@
 """Operators of the language model's serving layer, which reads the kept
-tokens: norm, 4-bit products, append to a paged cache, attention over it.
+tokens: norm, 4-bit products, append to a paged cache, attention over it; and
+those that keep the cache small: 4 bits, the tokens' accumulated weights, eviction.
 
 As in the rest of the binding, the functions only check and marshal torch
 tensors; here that part is compiled (csrc/binding.cpp), because a decode step
 is a handful of calls of a few microseconds each.  Each takes tensors of the
 current GPU, enqueues on torch's current stream (or ``stream``) and returns
 without waiting; outputs that are not given are allocated.  8-bit tensors are
-torch.float8_e4m3fn throughout.  Wrong types raise TypeError, wrong shapes,
+torch.float8_e4m3fn throughout, 4-bit caches uint8 (two codes a byte) with
+uint8 exponents of 32 dims each.  Wrong types raise TypeError, wrong shapes,
 strides and devices ValueError, what the library itself refuses
 CoverPruneError.  There are no backward passes: tensors that require a gradient
 raise ValueError, except under torch.no_grad().
@@ -20,7 +22,8 @@ import torch
 
 from . import HERE, CoverPruneError, library
 
-__all__ = ["rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention"]
+__all__ = ["rms_norm", "RmsNormResult", "w4_matvec", "kv_append", "paged_attention", "kv_append4", "kv_gather",
+           "paged_attention4", "paged_attention_mass", "kv_evict", "KvEvictResult"]
 
 
 class _Unloaded:
@@ -125,3 +128,97 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                                    out, lse, workspace)
     return _native.paged_attention(q, k_cache, v_cache, table, lengths, max_length, window, scale, k_scale, v_scale, return_lse,
                                    out, lse, workspace)
+
+
+def kv_append4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+               inv_freq: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+               v_scale: torch.Tensor, interleaved: bool = False, magnitude: float = 1.0, q_out: Optional[torch.Tensor] = None,
+               stream=None) -> Optional[torch.Tensor]:
+    """kv_append to a cache of 4 bits; returns the rotated queries (None without q).
+
+    Arguments as for kv_append, but the caches are uint8 [pages, heads,
+    page_size, d / 2], two codes a byte, with exponents k_scale and v_scale, uint8
+    [pages, heads, page_size, d / 32]; d is a multiple of 32.  Each 32 dims share a
+    power of two, the smallest that six times reaches their largest; codes are
+    0, .5, 1, 1.5, 2, 3, 4, 6 times it and a sign, to nearest."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_append4(q, k, v, positions, slots, inv_freq, k_cache, v_cache, k_scale, v_scale, interleaved, magnitude, q_out)
+    return _native.kv_append4(q, k, v, positions, slots, inv_freq, k_cache, v_cache, k_scale, v_scale, interleaved, magnitude, q_out)
+
+
+def kv_gather(k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, dtype: Optional[torch.dtype] = None,
+              k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None):
+    """Cached keys and values as dense rows: returns (k, v), [tokens, heads, d] each.
+
+    Caches and scales as kv_append and kv_append4 take them; slots [tokens] int64
+    (negative, or past the caches: zeros).  dtype: the caches' own type, and for 8
+    and 4 bits bfloat16 (default) or float16."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_gather(k_cache, v_cache, slots, dtype, k_scale, v_scale, k_out, v_out)
+    return _native.kv_gather(k_cache, v_cache, slots, dtype, k_scale, v_scale, k_out, v_out)
+
+
+def paged_attention4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                     table: torch.Tensor, lengths: torch.Tensor, max_length: Optional[int] = None, window: int = 0,
+                     scale: Optional[float] = None, return_lse: bool = False, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """paged_attention over a cache of 4 bits, as kv_append4 fills it (caches
+    [pages, heads, page_size, d / 2] and scales [pages, heads, page_size, d / 32], uint8)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return paged_attention4(q, k_cache, v_cache, k_scale, v_scale, table, lengths, max_length, window, scale, return_lse,
+                                    out, lse, workspace)
+    return _native.paged_attention4(q, k_cache, v_cache, k_scale, v_scale, table, lengths, max_length, window, scale, return_lse,
+                                    out, lse, workspace)
+
+
+def paged_attention_mass(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                         lengths: torch.Tensor, mass: torch.Tensor, max_length: Optional[int] = None, window: int = 0,
+                         scale: Optional[float] = None, k_scale: Optional[torch.Tensor] = None,
+                         v_scale: Optional[torch.Tensor] = None, return_lse: bool = False, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention over a cache of any type that also adds to each cached token's
+    mass the weight that it got; returns out, or (out, lse) with return_lse.
+
+    mass [batch, kv_heads, span] float32, span at least max_length, is updated in
+    place: mass[b, h, j] += sum over the query heads of h of softmax_j.  The
+    other arguments as for paged_attention; uint8 caches are 4-bit ones, their
+    scales the exponents.  max_length defaults to all that the table can hold, or
+    span where that is less."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return paged_attention_mass(q, k_cache, v_cache, table, lengths, mass, max_length, window, scale, k_scale, v_scale,
+                                        return_lse, out, lse, workspace)
+    return _native.paged_attention_mass(q, k_cache, v_cache, table, lengths, mass, max_length, window, scale, k_scale, v_scale,
+                                        return_lse, out, lse, workspace)
+
+
+class KvEvictResult(NamedTuple):
+    kept: torch.Tensor                 # [batch, kv_heads, keep] int32, the token now at each place; -1 past the new length
+    lengths: torch.Tensor              # [batch] int32, at most keep
+    mass: torch.Tensor                 # [batch, kv_heads, span] float32 in the new order, 0 past the new length
+
+
+def kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, mass: torch.Tensor,
+             keep: int, recent: int = 0, sink: int = 0, max_length: Optional[int] = None, k_scale: Optional[torch.Tensor] = None,
+             v_scale: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+             mass_out: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None, stream=None) -> KvEvictResult:
+    """Leave `keep` tokens of each sequence and head in the cache: the first
+    `sink`, the last `recent`, and of the others those of largest mass (as
+    paged_attention_mass adds it up).
+
+    The caches (and the exponents k_scale and v_scale of 4-bit ones) are updated
+    in place: kept tokens from place keep - recent on fill the places that fall vacant
+    before it, then the last `recent` follow in order.  A sequence's pages must be its
+    own.  mass_out may be mass itself; lengths_out may not be lengths.  Attention with a
+    window no longer goes by age afterwards."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_evict(k_cache, v_cache, table, lengths, mass, keep, recent, sink, max_length, k_scale, v_scale, kept, mass_out,
+                            lengths_out, workspace)
+    return KvEvictResult._make(_native.kv_evict(k_cache, v_cache, table, lengths, mass, keep, recent, sink, max_length, k_scale,
+                                                v_scale, kept, mass_out, lengths_out, workspace))
