@@ -1,19 +1,28 @@
 // Eviction from a paged cache: of each sequence and key-value head the tokens of
 // largest mass stay, and close the gaps that the others leave.
 //
-// With n tokens of which m = keep stay (n > keep), the first `sink` and the last
-// `recent` among them, f = m - recent.  Tokens below f that stay do not move; those
-// from f to n - recent move to the places below f that fall vacant, in order; the
-// last `recent` go to f and on, in order.  So the rows that move are at most as
-// many as those that leave, and the last ones, and not the whole cache.
+// With n tokens of which keep stay (n > keep), the first `sink` and the last
+// `recent` among them, front = keep - recent.  Tokens below the front that stay do not
+// move; those from it to n - recent move to the places below it that fall vacant, in
+// order; the last `recent` go to the front and on, in order.  So the rows that move are
+// at most as many as those that leave, and the last ones, and not the whole cache.
 //
-//   select  a block a (sequence, head): the mass of rank m - sink - recent by its
-//           bits, eight at a time; then, in order of the tokens, who leaves, who
-//           moves and the new order.
-//   move    rows to vacant places, and the new masses.  All come from f on and
-//           go below f, so no row is read after it was written.
-//   shift   the last rows, once the places at f are empty; in ascending runs, each
-//           read whole before it is written, since they may overlap.
+// Who stays: of the tokens in [sink, n - recent) the want = front - sink of largest
+// rank (a mass as a whole number in the order of masses), found digit by digit from
+// counts of them; of those at the last rank the earlier.  The order of tokens comes
+// from counts as well, so nothing depends on the order of atomics.
+//
+//   evict_few    where few rows move, all of it by a block a (sequence, head), the
+//                ranks in LDS
+//   otherwise, with a sequence's tokens in up to 64 chunks:
+//   evict_count  a chunk's counts of the rank's highest 10 bits
+//   evict_bucket the value of those at which the rank wanted lies; a chunk's tokens that
+//                have it, its counts of those above
+//   evict_border the rank itself, from the tokens with that value, by every block for
+//                itself; then its chunk's vacant places and movers
+//   evict_move   rows and masses to vacant places.  All come from the front on and go
+//                below it, so no row is read after it was written.
+//   evict_shift  the last rows, once the places at the front are empty
 #include <algorithm>
 
 #include "launch.h"
@@ -22,25 +31,7 @@
 namespace cp {
 namespace {
 
-constexpr int kSelect = 1024;
-
-// Where the workspace holds what, for each (sequence, head), in 32-bit words.
-struct Lists {
-  int64_t places;                 // most places that can fall vacant
-  int64_t vacant, movers, count, mass, stride;
-};
-__host__ __device__ inline Lists lists_of(int64_t keep, int64_t recent, int64_t max_length) {
-  Lists l;
-  const int64_t a = keep - recent, b = max_length - keep;
-  l.places = a < b ? a : b;
-  if (l.places < 0) l.places = 0;
-  l.count = 0;
-  l.vacant = 1;
-  l.movers = l.vacant + l.places;
-  l.mass = l.movers + l.places;
-  l.stride = l.mass + (keep < max_length ? keep : max_length);
-  return l;
-}
+constexpr int kSelect = 1024, kWaves = kSelect / kWave;
 
 // A mass as a number in the order of masses: NaN lowest, -0 as 0.
 __device__ __forceinline__ uint32_t rank_of(float m) {
@@ -49,155 +40,531 @@ __device__ __forceinline__ uint32_t rank_of(float m) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Sum of one number a thread over the block's lower threads, and over all.
-__device__ __forceinline__ int block_scan(int x, int* s_part, int* total) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int sum = x;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(sum, o);
-    if (lane >= o) sum += y;
-  }
-  if (lane == kWave - 1) s_part[wave] = sum;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < kSelect / kWave; ++i) {
-    const int v = s_part[i];
-    if (i < wave) before += v;
-    all += v;
-  }
-  __syncthreads();
-  *total = all;
-  return before + sum - x;
-}
-
 __device__ __forceinline__ int tokens_of(const KvEvictParams& p, int b) { return max(0, int(min(int64_t(p.lengths[b]), p.max_length))); }
 
-__global__ __launch_bounds__(kSelect) void evict_select_kernel(KvEvictParams p) {
-  __shared__ int s_hist[256];
-  __shared__ int s_part[kSelect / kWave];
-  __shared__ uint32_t s_digit, s_left;
-  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink);
-  const int64_t head = int64_t(b) * p.hk + kh;
-  const Lists l = lists_of(p.keep, p.recent, p.max_length);
-  uint32_t* ws = static_cast<uint32_t*>(p.workspace) + head * l.stride;
-  int *vacant = reinterpret_cast<int*>(ws + l.vacant), *movers = reinterpret_cast<int*>(ws + l.movers);
-  float* fresh = reinterpret_cast<float*>(ws + l.mass);
-  const float* mass = p.mass + head * p.span;
-  int32_t* kept = p.kept + head * p.keep;
-  if (n <= keep) {
-    for (int64_t j = tid; j < keep; j += kSelect) {
-      kept[j] = j < n ? int(j) : -1;
-      if (j < n) fresh[j] = mass[j];
-    }
-    if (tid == 0) ws[l.count] = 0u;
-    return;
-  }
-  // Of the tokens in [sink, end) `want` stay: those whose rank is above `border`, and
-  // the first `ties` of those at it.
-  const int end = n - recent, want = keep - recent - sink, front = keep - recent;
-  uint32_t border = 0u;
-  int ties = 0;
-  if (want > 0) {
-    uint32_t left = uint32_t(want);
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelect) s_hist[i] = 0;
-      __syncthreads();
-      for (int j = sink + tid; j < end; j += kSelect) {
-        const uint32_t r = rank_of(mass[j]);
-        if (shift == 24 || r >> (shift + 8) == border >> (shift + 8)) atomicAdd(&s_hist[r >> shift & 255u], 1);
-      }
-      __syncthreads();
-      // The digit at which the counts from the highest on reach what is left.
-      if (tid < kWave) {
-        int c[4], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += c[i] = s_hist[255 - (tid * 4 + i)];
-        int upto = sum;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-          const int y = __shfl_up(upto, o);
-          if (tid >= o) upto += y;
-        }
-        int before = upto - sum;
-        if (before < int(left) && int(left) <= upto) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (before < int(left) && int(left) <= before + c[i]) {
-              s_digit = 255 - (tid * 4 + i);
-              s_left = left - before;
-            }
-            before += c[i];
-          }
-        }
-      }
-      __syncthreads();
-      border |= s_digit << shift;
-      left = s_left;
-      __syncthreads();
-    }
-    ties = int(left);
-  }
-  // In order: counts of ties, vacant places and movers up to each token.
-  int seen = 0, gaps = 0, moved = 0;
-  for (int j0 = 0; j0 < end; j0 += kSelect) {
-    const int j = j0 + tid;
-    const bool here = j < end;
-    const float m = here ? mass[j] : 0.f;
-    const uint32_t r = rank_of(m);
-    const bool inner = here && j >= sink;
-    const bool tie = inner && want > 0 && r == border;
-    int total;
-    const int rank = seen + block_scan(tie, s_part, &total);
-    seen += total;
-    const bool stays = here && (j < sink || (want > 0 && (r > border || (tie && rank < ties))));
-    const bool gap = here && !stays && j < front, goes = stays && j >= front;
-    // Both counts in one number: below the front only gaps, from it on only movers,
-    // but for the run in which it lies.
-    int both;
-    const int at = block_scan(gap | int(goes) << 16, s_part, &both);
-    if (gap) vacant[gaps + (at & 0xffff)] = j;
-    if (goes) movers[moved + (at >> 16)] = j;
-    gaps += both & 0xffff;
-    moved += both >> 16;
-    if (stays && j < front) {
-      kept[j] = j;
-      fresh[j] = m;
-    }
-  }
-  __syncthreads();
-  for (int i = tid; i < gaps; i += kSelect) {
-    const int from = movers[i], to = vacant[i];
-    kept[to] = from;
-    fresh[to] = mass[from];
-  }
-  for (int i = tid; i < recent; i += kSelect) {
-    kept[front + i] = end + i;
-    fresh[front + i] = mass[end + i];
-  }
-  if (tid == 0) ws[l.count] = uint32_t(gaps);
+// A workgroup barrier that orders LDS alone: what goes to and from memory stays under way.
+__device__ __forceinline__ void lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// One row of codes, values or exponents from one place to another, `units` of U, one of them.
+// How many lanes below this one have their bit in `ballot`.
+__device__ __forceinline__ int lanes_below(unsigned long long ballot) {
+  return int(__builtin_amdgcn_mbcnt_hi(unsigned(ballot >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(ballot), 0u)));
+}
+
+// Sum over this lane and the lower ones.
+__device__ __forceinline__ int wave_upto(int x) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// counts[bins * COPIES]: the digit at which the counts from the highest on reach `left`
+// (1 <= left <= their sum), and how many are left at it.  By one wave; bins a multiple of 64.
+template <int BINS, int COPIES>
+__device__ __forceinline__ void find_digit(const int* counts, int left, uint32_t* digit, int* rest) {
+  constexpr int kPer = BINS / kWave;
+  const int lane = threadIdx.x % kWave, top = BINS - 1 - lane * kPer;
+  int sum = 0;
+#pragma unroll 4
+  for (int i = 0; i < kPer * COPIES; ++i) sum += counts[(top - kPer + 1) * COPIES + i];
+  const int upto = wave_upto(sum);
+  int before = upto - sum;
+  if (before < left && left <= upto) {
+    for (int i = 0; i < kPer; ++i) {
+      int c = 0;
+      for (int e = 0; e < COPIES; ++e) c += counts[(top - i) * COPIES + e];
+      if (left <= before + c) {
+        *digit = uint32_t(top - i);
+        *rest = left - before;
+        break;
+      }
+      before += c;
+    }
+  }
+}
+
+// Rows of a sequence and head.
 struct Place {
   const KvEvictParams& p;
   int b, kh;
   // Row of token t.
-  __device__ __forceinline__ int64_t row(int t) const {
+  __device__ __forceinline__ uint32_t row(int t) const {
     const int page = t / p.page;
     const unsigned entry = min(unsigned(p.table[int64_t(b) * p.width + page]), unsigned(p.pages - 1));
-    return (int64_t(entry) * p.hk + kh) * p.page + (t - page * p.page);
+    return (entry * unsigned(p.hk) + unsigned(kh)) * unsigned(p.page) + unsigned(t - page * p.page);
   }
 };
 
-// The rows' copies: `lanes` threads a pair of places.
-constexpr int kMoveRows = 32;
+// Moves first, first + step, ... of `moves` rows from one place to another by a block of
+// `threads`: 2^shift threads have a key's `units` units, then a value's, and four moves
+// at a time.  places(move, to, from) gives the rows.  IN_ORDER: rows may overlap their
+// new places; a lower move's row is read before a higher one's is written.
+template <bool IN_ORDER, class X, class Places>
+__device__ __forceinline__ void copy_rows(X* keys, X* values, int units, int shift, int threads, int moves, int first, int step, Places places) {
+  const int lanes = 1 << shift, u0 = int(threadIdx.x) & (lanes - 1), per = threads >> shift;
+  const int mine = int(threadIdx.x) >> shift;
+  for (int64_t i0 = int64_t(first) * 4 * per; i0 < moves; i0 += int64_t(step) * 4 * per) {
+    uint32_t to[4], from[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t i = i0 + e * per + mine;
+      if (i < moves) places(int(i), &to[e], &from[e]);
+    }
+    // (One turn but for rows of over 64 units.)
+    for (int u = u0; IN_ORDER ? u - u0 < 2 * units : u < 2 * units; u += lanes) {
+      X* base = u < units ? keys : values;
+      const int v = u < units ? u : u - units;
+      X x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (u < 2 * units && i0 + e * per + mine < moves) x[e] = base[int64_t(from[e]) * units + v];
+      if (IN_ORDER) __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (u < 2 * units && i0 + e * per + mine < moves) base[int64_t(to[e]) * units + v] = x[e];
+      if (IN_ORDER) __syncthreads();
+    }
+  }
+}
+
+// All of them: keys, values and exponents.
+template <bool IN_ORDER, class U, class Places>
+__device__ __forceinline__ void copy_moves(const KvEvictParams& p, int threads, int moves, int first, int step, Places places) {
+  copy_rows<IN_ORDER>(static_cast<U*>(p.k_cache), static_cast<U*>(p.v_cache), p.row_bytes / int(sizeof(U)), p.row_shift, threads, moves,
+                      first, step, places);
+  if (p.exp_bytes == 0) return;
+  if (p.exp_words)
+    copy_rows<IN_ORDER>(reinterpret_cast<uint32_t*>(p.k_exps), reinterpret_cast<uint32_t*>(p.v_exps), p.exp_bytes / 4, p.exp_shift,
+                        threads, moves, first, step, places);
+  else
+    copy_rows<IN_ORDER>(p.k_exps, p.v_exps, p.exp_bytes, p.exp_shift, threads, moves, first, step, places);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: one launch.
+
+constexpr int kFewTokens = 16384;   // whose ranks are in LDS
+constexpr int kFewRows = 2048;      // that move: vacant places and `recent`
+constexpr int kCopies = 8;          // of each count: most masses share their highest bits, and
+                                    // additions to one address wait for each other
+
 template <class U>
-__device__ __forceinline__ void copy_row(void* base, int64_t to, int64_t from, int units, int lane, int lanes) {
-  U* x = static_cast<U*>(base);
-  for (int i = lane; i < units; i += lanes) x[to * units + i] = x[from * units + i];
+__global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
+  extern __shared__ uint32_t s_rank[];                      // [max_length]
+  __shared__ int s_hist[2][256 * kCopies];
+  __shared__ uint32_t s_to[kFewRows], s_from[kFewRows];     // tokens, then their rows
+  __shared__ uint32_t s_digit;
+  __shared__ int s_left, s_ties[kWaves], s_both[kWaves];
+  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink), m = min(n, keep);
+  const int64_t head = int64_t(b) * p.hk + kh;
+  const float* mass = p.mass + head * p.span;
+  float* out = p.mass_out + head * p.span;
+  int32_t* kept = p.kept + head * p.keep;
+  if (kh == 0 && tid == 0) p.lengths_out[b] = m;
+  if (n <= keep) {
+    for (int64_t j = tid; j < keep; j += kSelect) kept[j] = j < n ? int(j) : -1;
+    for (int64_t j = tid; j < p.span; j += kSelect) out[j] = j < n ? mass[j] : 0.f;
+    return;
+  }
+  const int end = n - recent, front = keep - recent, want = front - sink;
+  for (int i = tid; i < 2 * 256 * kCopies; i += kSelect) s_hist[0][i] = 0;
+#pragma unroll 4
+  for (int j = tid; j < end; j += kSelect) s_rank[j] = rank_of(mass[j]);
+  lds_sync();
+  uint32_t border = 0u;
+  int ties = want;
+  if (want > 0) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      int* hist = s_hist[shift / 8 % 2];
+#pragma unroll 4
+      for (int j = sink + tid; j < end; j += kSelect) {
+        const uint32_t r = s_rank[j];
+        // (In two steps, so that nothing is left of them the first time.)
+        if ((r ^ border) >> shift >> 8 == 0u) atomicAdd(&hist[(r >> shift & 255u) * kCopies + lane % kCopies], 1);
+      }
+      lds_sync();
+      if (wave == 0) find_digit<256, kCopies>(hist, ties, &s_digit, &s_left);
+      lds_sync();
+      border |= s_digit << shift;
+      ties = s_left;
+      for (int i = tid; i < 256 * kCopies; i += kSelect) hist[i] = 0;
+    }
+  }
+  // Each wave has consecutive tokens: how many are at the border, then how many places
+  // fall vacant below the front and how many tokens from it on stay.
+  const int run = (end + kSelect - 1) / kSelect * kWave, j0 = wave * run, j1 = min(end, j0 + run);
+  int equal = 0;
+  for (int j = j0 + lane; j < j1; j += kWave) equal += __popcll(__ballot(want > 0 && j >= sink && s_rank[j] == border));
+  if (lane == 0) s_ties[wave] = j0 < j1 ? equal : 0;
+  lds_sync();
+  int tie0 = 0;
+  for (int w = 0; w < wave; ++w) tie0 += s_ties[w];
+  // Token j (every lane of the wave comes along): whether it stays; `seen` counts ties.
+  auto stays = [&](int j, int& seen) {
+    const bool here = j < j1;
+    const uint32_t r = here ? s_rank[j] : 0u;
+    const bool tie = here && want > 0 && j >= sink && r == border;
+    const unsigned long long all = __ballot(tie);
+    const bool yes = here && (j < sink || (want > 0 && (r > border || (tie && seen + lanes_below(all) < ties))));
+    seen += __popcll(all);
+    return yes;
+  };
+  int seen = tie0, gaps = 0, goes = 0;
+  for (int t = j0; t < j1; t += kWave) {
+    const int j = t + lane;
+    const bool yes = stays(j, seen);
+    gaps += __popcll(__ballot(j < j1 && !yes && j < front));
+    goes += __popcll(__ballot(yes && j >= front));
+  }
+  if (lane == 0) s_both[wave] = gaps | goes << 16;
+  lds_sync();
+  int both = 0, total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    const int v = s_both[w];
+    if (w < wave) both += v;
+    total += v;
+  }
+  total &= 0xffff;
+  int gap_at = both & 0xffff, go_at = both >> 16;
+  seen = tie0;
+  for (int t = j0; t < j1; t += kWave) {
+    const int j = t + lane;
+    const bool yes = stays(j, seen), gap = j < j1 && !yes && j < front, go = yes && j >= front;
+    const unsigned long long all_gaps = __ballot(gap), all_go = __ballot(go);
+    if (yes && !go) {
+      kept[j] = j;
+      if (out != mass) out[j] = mass[j];
+    }
+    if (gap) s_to[gap_at + lanes_below(all_gaps)] = j;
+    if (go) s_from[go_at + lanes_below(all_go)] = j;
+    gap_at += __popcll(all_gaps);
+    go_at += __popcll(all_go);
+  }
+  const int moves = total + recent;
+  for (int i = total + tid; i < moves; i += kSelect) {
+    s_to[i] = front + i - total;
+    s_from[i] = end + i - total;
+  }
+  lds_sync();
+  // The masses like the rows: first those that go below the front, then the last ones in
+  // ascending runs, each read whole before it is written.
+  for (int i = tid; i < moves; i += kSelect) kept[s_to[i]] = s_from[i];
+  for (int i = tid; i < total; i += kSelect) out[s_to[i]] = mass[s_from[i]];
+  for (int i0 = total; i0 < moves; i0 += kSelect) {
+    const int i = i0 + tid;
+    const float v = i < moves ? mass[s_from[i]] : 0.f;
+    __syncthreads();
+    if (i < moves) out[s_to[i]] = v;
+  }
+  __syncthreads();
+  for (int64_t j = m + tid; j < p.span; j += kSelect) out[j] = 0.f;
+  const Place place = {p, b, kh};
+  for (int i = tid; i < moves; i += kSelect) {
+    s_to[i] = place.row(s_to[i]);
+    s_from[i] = place.row(s_from[i]);
+  }
+  lds_sync();
+  copy_moves<false, U>(p, kSelect, total, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
+    *to = s_to[i];
+    *from = s_from[i];
+  });
+  if (recent == 0) return;
+  __syncthreads();
+  copy_moves<true, U>(p, kSelect, recent, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
+    *to = s_to[total + i];
+    *from = s_from[total + i];
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Many rows.
+
+constexpr int kBuckets = 1024;      // of the rank's highest 10 bits
+constexpr int kRest = 22 - 11;      // its other bits in two digits of 11
+
+// Where the workspace holds what, for each (sequence, head), in 32-bit words.
+struct Lists {
+  int chunks, chunk;                // tokens a chunk, a multiple of kSelect
+  int64_t places;                   // most places that can fall vacant
+  int64_t hist, stats, some, vacant, movers, mover_mass, mass, ties, gaps, stride;
+};
+__host__ __device__ inline Lists lists_of(int64_t keep, int64_t recent, int64_t max_length) {
+  Lists l;
+  const int64_t a = keep - recent, b = max_length - keep;
+  l.places = a < b ? a : b;
+  if (l.places < 0) l.places = 0;
+  const int64_t least = (max_length + 63) / 64;
+  l.chunk = int(((least > 4096 ? least : 4096) + kSelect - 1) / kSelect * kSelect);
+  l.chunks = int((max_length + l.chunk - 1) / l.chunk);
+  l.hist = 0;
+  l.stats = l.hist + int64_t(l.chunks) * kBuckets;    // a chunk's tokens in the bucket, above it below the front, above it from there on
+  l.some = l.stats + int64_t(l.chunks) * 4;           // tokens in the bucket, a chunk's from its first token's place on
+  l.vacant = l.some + int64_t(l.chunks) * l.chunk;
+  l.movers = l.vacant + l.places;
+  l.mover_mass = l.movers + l.places;
+  l.mass = l.mover_mass + l.places;
+  l.ties = l.mass + (keep < max_length ? keep : max_length);
+  l.gaps = l.ties + 1;
+  l.stride = l.gaps + 1;
+  return l;
+}
+
+// What the blocks of a (sequence, head) share.
+struct Chunk {
+  Lists l;
+  int64_t head;
+  int kh, b, n, end, front, sink, want, j0, j1, per, w0, w1;
+  const float* mass;
+  uint32_t* ws;
+
+  __device__ __forceinline__ Chunk(const KvEvictParams& p) : l(lists_of(p.keep, p.recent, p.max_length)) {
+    kh = blockIdx.y;
+    b = blockIdx.z;
+    head = int64_t(b) * p.hk + kh;
+    n = tokens_of(p, b);
+    sink = int(p.sink);
+    front = int(p.keep - p.recent);
+    want = front - sink;
+    end = n > p.keep ? n - int(p.recent) : 0;
+    j0 = min(end, int(blockIdx.x) * l.chunk);
+    j1 = min(end, j0 + l.chunk);
+    mass = p.mass + head * p.span;
+    ws = static_cast<uint32_t*>(p.workspace) + head * l.stride;
+    // This wave's tokens of the chunk.
+    per = l.chunk / kWaves;
+    w0 = min(j1, j0 + int(threadIdx.x) / kWave * per);
+    w1 = min(j1, w0 + per);
+  }
+};
+
+__global__ __launch_bounds__(kSelect) void evict_count_kernel(KvEvictParams p) {
+  __shared__ int s_hist[kBuckets * 4];
+  const Chunk c(p);
+  const int tid = threadIdx.x;
+  if (c.end == 0) return;
+  for (int i = tid; i < kBuckets * 4; i += kSelect) s_hist[i] = 0;
+  lds_sync();
+#pragma unroll 4
+  for (int j = max(c.j0, c.sink) + tid; j < c.j1; j += kSelect) atomicAdd(&s_hist[(rank_of(c.mass[j]) >> 22) * 4 + tid % 4], 1);
+  lds_sync();
+  c.ws[c.l.hist + int64_t(blockIdx.x) * kBuckets + tid] = s_hist[tid * 4] + s_hist[tid * 4 + 1] + s_hist[tid * 4 + 2] + s_hist[tid * 4 + 3];
+}
+
+__global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) {
+  __shared__ int s_hist[kBuckets];
+  __shared__ int s_part[3][kWaves];
+  __shared__ uint32_t s_digit;
+  __shared__ int s_left;
+  const Chunk c(p);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  if (c.end == 0 || c.want == 0) return;
+  int sum = 0;
+#pragma unroll 8
+  for (int i = 0; i < c.l.chunks; ++i) sum += int(c.ws[c.l.hist + int64_t(i) * kBuckets + tid]);
+  s_hist[tid] = sum;
+  lds_sync();
+  if (wave == 0) find_digit<kBuckets, 1>(s_hist, c.want, &s_digit, &s_left);
+  lds_sync();
+  const uint32_t bucket = s_digit;
+  int in = 0, low = 0, high = 0;
+  for (int t = c.w0; t < c.w1; t += kWave) {
+    const int j = t + lane;
+    const bool here = j < c.w1 && j >= c.sink;
+    const uint32_t top = here ? rank_of(c.mass[j]) >> 22 : 0u;
+    in += __popcll(__ballot(here && top == bucket));
+    low += __popcll(__ballot(here && top > bucket && j < c.front));
+    high += __popcll(__ballot(here && top > bucket && j >= c.front));
+  }
+  if (lane == 0) {
+    s_part[0][wave] = in;
+    s_part[1][wave] = low;
+    s_part[2][wave] = high;
+  }
+  lds_sync();
+  int at = 0;
+  for (int w = 0; w < wave; ++w) at += s_part[0][w];
+  uint32_t* some = c.ws + c.l.some + c.j0;
+  for (int t = c.w0; t < c.w1; t += kWave) {
+    const int j = t + lane;
+    const bool here = j < c.w1 && j >= c.sink;
+    const uint32_t r = here ? rank_of(c.mass[j]) : 0u;
+    const bool yes = here && r >> 22 == bucket;
+    const unsigned long long all = __ballot(yes);
+    // The rank's other 22 bits, and whether it is below the front.
+    if (yes) some[at + lanes_below(all)] = (r & 0x3fffffu) | uint32_t(j < c.front) << 31;
+    at += __popcll(all);
+  }
+  if (tid < 4) {
+    int x = int(bucket);
+    if (tid < 3) {
+      x = 0;
+      for (int w = 0; w < kWaves; ++w) x += s_part[tid][w];
+    }
+    c.ws[c.l.stats + int64_t(blockIdx.x) * 4 + tid] = uint32_t(x);
+  }
+  // (Every block finds the same; the first leaves it.)
+  if (blockIdx.x == 0 && tid == 0) c.ws[c.l.ties] = uint32_t(s_left);
+}
+
+__global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) {
+  __shared__ int s_hist[2048 * 4];
+  __shared__ uint32_t s_digit;
+  __shared__ int s_left;
+  __shared__ int s_equal[64], s_low[64], s_high[64], s_equal_low[64];
+  __shared__ int s_part[kWaves], s_both[2][kWaves];
+  const Chunk c(p);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int32_t* kept = p.kept + c.head * p.keep;
+  float* fresh = reinterpret_cast<float*>(c.ws + c.l.mass);
+  if (c.end == 0) {
+    // All stay.
+    for (int64_t j = int64_t(blockIdx.x) * kSelect + tid; j < p.keep; j += int64_t(gridDim.x) * kSelect) {
+      kept[j] = j < c.n ? int(j) : -1;
+      if (j < c.n) fresh[j] = c.mass[j];
+    }
+    return;
+  }
+  const uint32_t* stats = c.ws + c.l.stats;
+  uint32_t border = 0u;
+  int ties = 0;
+  if (c.want > 0) {
+    const uint32_t bucket = stats[3];
+    ties = int(c.ws[c.l.ties]);
+    uint32_t low = 0u;
+#pragma unroll 1
+    for (int shift = kRest; shift >= 0; shift -= kRest) {
+      for (int i = tid; i < 2048 * 4; i += kSelect) s_hist[i] = 0;
+      lds_sync();
+      // A wave takes every 16th chunk's tokens of the bucket.
+      for (int k = wave; k < c.l.chunks; k += kWaves) {
+        const int count = int(stats[k * 4]);
+        const uint32_t* some = c.ws + c.l.some + int64_t(k) * c.l.chunk;
+#pragma unroll 4
+        for (int i = lane; i < count; i += kWave) {
+          const uint32_t r = some[i] & 0x3fffffu;
+          if (shift == kRest || r >> kRest == low >> kRest) atomicAdd(&s_hist[(r >> shift & 2047u) * 4 + lane % 4], 1);
+        }
+      }
+      lds_sync();
+      if (wave == 0) find_digit<2048, 4>(s_hist, ties, &s_digit, &s_left);
+      lds_sync();
+      low |= s_digit << shift;
+      ties = s_left;
+    }
+    border = bucket << 22 | low;
+    // Each chunk's tokens at the border and above it.
+    for (int k = wave; k < c.l.chunks; k += kWaves) {
+      const int count = int(stats[k * 4]);
+      const uint32_t* some = c.ws + c.l.some + int64_t(k) * c.l.chunk;
+      int equal = 0, equal_low = 0, above_low = int(stats[k * 4 + 1]), above_high = int(stats[k * 4 + 2]);
+      for (int i0 = 0; i0 < count; i0 += kWave) {
+        const bool here = i0 + lane < count;
+        const uint32_t v = here ? some[i0 + lane] : 0u, r = v & 0x3fffffu;
+        const bool below = v >> 31 != 0u;
+        equal += __popcll(__ballot(here && r == low));
+        equal_low += __popcll(__ballot(here && r == low && below));
+        above_low += __popcll(__ballot(here && r > low && below));
+        above_high += __popcll(__ballot(here && r > low && !below));
+      }
+      if (lane == 0) {
+        s_equal[k] = equal;
+        s_equal_low[k] = equal_low;
+        s_low[k] = above_low;
+        s_high[k] = above_high;
+      }
+    }
+  } else if (tid < c.l.chunks) {
+    s_equal[tid] = s_equal_low[tid] = s_low[tid] = s_high[tid] = 0;
+  }
+  lds_sync();
+  // Up to this chunk: ties, vacant places, movers.  And all vacant places.
+  int tie0 = 0, gap0 = 0, go0 = 0, gaps = 0;
+  {
+    int seen = 0;
+    for (int k = 0; k < c.l.chunks; ++k) {
+      const int a = k * c.l.chunk, z = min(c.front, min(c.end, a + c.l.chunk));
+      const int taken = min(max(ties - seen, 0), s_equal[k]), taken_low = min(taken, s_equal_low[k]);
+      const int sinks = min(max(c.sink - a, 0), c.l.chunk);
+      if (k < int(blockIdx.x)) {
+        tie0 += s_equal[k];
+        go0 += s_high[k] + taken - taken_low;
+      }
+      gaps += max(z - a, 0) - (sinks + s_low[k] + taken_low);
+      if (k < int(blockIdx.x)) gap0 = gaps;
+      seen += s_equal[k];
+    }
+  }
+  auto rank = [&](int j) { return rank_of(c.mass[j]); };
+  int equal = 0;
+  for (int t = c.w0; t < c.w1; t += kWave) {
+    const int j = t + lane;
+    equal += __popcll(__ballot(j < c.w1 && c.want > 0 && j >= c.sink && rank(j) == border));
+  }
+  if (lane == 0) s_part[wave] = equal;
+  lds_sync();
+  for (int w = 0; w < wave; ++w) tie0 += s_part[w];
+  auto stays = [&](int j, float m, int& seen) {
+    const bool here = j < c.w1;
+    const uint32_t r = rank_of(m);
+    const bool tie = here && c.want > 0 && j >= c.sink && r == border;
+    const unsigned long long all = __ballot(tie);
+    const bool yes = here && (j < c.sink || (c.want > 0 && (r > border || (tie && seen + lanes_below(all) < ties))));
+    seen += __popcll(all);
+    return yes;
+  };
+  int seen = tie0, my_gaps = 0, my_go = 0;
+  for (int t = c.w0; t < c.w1; t += kWave) {
+    const int j = t + lane;
+    const bool yes = stays(j, j < c.w1 ? c.mass[j] : 0.f, seen);
+    my_gaps += __popcll(__ballot(j < c.w1 && !yes && j < c.front));
+    my_go += __popcll(__ballot(yes && j >= c.front));
+  }
+  if (lane == 0) {
+    s_both[0][wave] = my_gaps;
+    s_both[1][wave] = my_go;
+  }
+  lds_sync();
+  for (int w = 0; w < wave; ++w) {
+    gap0 += s_both[0][w];
+    go0 += s_both[1][w];
+  }
+  int *vacant = reinterpret_cast<int*>(c.ws + c.l.vacant), *movers = reinterpret_cast<int*>(c.ws + c.l.movers);
+  float* mover_mass = reinterpret_cast<float*>(c.ws + c.l.mover_mass);
+  seen = tie0;
+  for (int t = c.w0; t < c.w1; t += kWave) {
+    const int j = t + lane;
+    const float m = j < c.w1 ? c.mass[j] : 0.f;
+    const bool yes = stays(j, m, seen), gap = j < c.w1 && !yes && j < c.front, go = yes && j >= c.front;
+    const unsigned long long all_gaps = __ballot(gap), all_go = __ballot(go);
+    if (yes && !go) {
+      kept[j] = j;
+      fresh[j] = m;
+    }
+    if (gap) {
+      kept[j] = -1;                 // until evict_move fills it
+      vacant[gap0 + lanes_below(all_gaps)] = j;
+    }
+    if (go) {
+      const int at = go0 + lanes_below(all_go);
+      movers[at] = j;
+      mover_mass[at] = m;
+    }
+    gap0 += __popcll(all_gaps);
+    go0 += __popcll(all_go);
+  }
+  for (int i = int(blockIdx.x) * kSelect + tid; i < p.recent; i += int(gridDim.x) * kSelect) {
+    kept[c.front + i] = c.end + i;
+    fresh[c.front + i] = c.mass[c.end + i];
+  }
+  if (blockIdx.x == 0 && tid == 0) c.ws[c.l.gaps] = uint32_t(gaps);
 }
 
 template <class U>
@@ -206,83 +573,97 @@ __global__ __launch_bounds__(256) void evict_move_kernel(KvEvictParams p) {
   const int64_t head = int64_t(b) * p.hk + kh;
   const Lists l = lists_of(p.keep, p.recent, p.max_length);
   const uint32_t* ws = static_cast<const uint32_t*>(p.workspace) + head * l.stride;
-  const int count = int(ws[l.count]);
+  const int n = tokens_of(p, b), m = min(int64_t(n), p.keep), gaps = n > m ? int(ws[l.gaps]) : 0;
   const int *vacant = reinterpret_cast<const int*>(ws + l.vacant), *movers = reinterpret_cast<const int*>(ws + l.movers);
-  const float* fresh = reinterpret_cast<const float*>(ws + l.mass);
-  const int n = tokens_of(p, b), m = min(int64_t(n), p.keep);
+  const float *mover_mass = reinterpret_cast<const float*>(ws + l.mover_mass), *fresh = reinterpret_cast<const float*>(ws + l.mass);
   float* mass = p.mass_out + head * p.span;
-  for (int64_t j = int64_t(blockIdx.x) * 256 + tid; j < p.span; j += int64_t(gridDim.x) * 256) mass[j] = j < m ? fresh[j] : 0.f;
-  if (kh == 0 && blockIdx.x == 0 && tid == 0) p.lengths_out[b] = m;
-  const Place place = {p, b, kh};
-  const int units = p.row_bytes / int(sizeof(U));
-  const int lane = tid % 8, group = tid / 8;
-  for (int i = blockIdx.x * kMoveRows + group; i < count; i += int(gridDim.x) * kMoveRows) {
-    const int64_t to = place.row(vacant[i]), from = place.row(movers[i]);
-    copy_row<U>(p.k_cache, to, from, units, lane, 8);
-    copy_row<U>(p.v_cache, to, from, units, lane, 8);
-    if (p.exp_bytes) {
-      copy_row<uint8_t>(p.k_exps, to, from, p.exp_bytes, lane, 8);
-      copy_row<uint8_t>(p.v_exps, to, from, p.exp_bytes, lane, 8);
-    }
+  int32_t* kept = p.kept + head * p.keep;
+  const int front = n > m ? int(p.keep - p.recent) : m;
+  const int first = int(blockIdx.x) * 256 + tid, step = int(gridDim.x) * 256;
+  for (int64_t j = first; j < p.span; j += step) {
+    // A vacant place's mass comes below.
+    if (j >= front || kept[j] == j) mass[j] = j < m ? fresh[j] : 0.f;
   }
+  for (int i = first; i < gaps; i += step) {
+    mass[vacant[i]] = mover_mass[i];
+    kept[vacant[i]] = movers[i];
+  }
+  if (kh == 0 && first == 0) p.lengths_out[b] = m;
+  const Place place = {p, b, kh};
+  copy_moves<false, U>(p, 256, gaps, blockIdx.x, gridDim.x, [&](int i, uint32_t* to, uint32_t* from) {
+    *to = place.row(vacant[i]);
+    *from = place.row(movers[i]);
+  });
 }
 
 template <class U>
-__global__ __launch_bounds__(256) void evict_shift_kernel(KvEvictParams p) {
-  const int kh = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent);
+__global__ __launch_bounds__(kSelect) void evict_shift_kernel(KvEvictParams p) {
+  const int n = tokens_of(p, blockIdx.z), keep = int(p.keep), recent = int(p.recent);
   if (n <= keep) return;
-  const Place place = {p, b, kh};
-  // Block x has the keys, the values, or the exponents of either.
-  void* base = blockIdx.x == 0 ? p.k_cache : blockIdx.x == 1 ? p.v_cache : blockIdx.x == 2 ? static_cast<void*>(p.k_exps) : static_cast<void*>(p.v_exps);
-  const int units = blockIdx.x < 2 ? p.row_bytes / int(sizeof(U)) : p.exp_bytes;
-  // Units in the order of rows: a run of 256 is read before any of it is written, and
-  // a later run's rows lie behind all rows written so far.
-  const int64_t total = int64_t(recent) * units;
-  for (int64_t i0 = 0; i0 < total; i0 += 256) {
-    const int64_t i = i0 + tid;
-    const bool here = i < total;
-    const int r = here ? int(i / units) : 0, u = here ? int(i - int64_t(r) * units) : 0;
-    const int64_t from = place.row(n - recent + r) * units + u, to = place.row(keep - recent + r) * units + u;
-    U x;
-    uint8_t e = 0;
-    if (here) {
-      if (blockIdx.x < 2) x = static_cast<const U*>(base)[from];
-      else e = static_cast<const uint8_t*>(base)[from];
-    }
-    __syncthreads();
-    if (here) {
-      if (blockIdx.x < 2) static_cast<U*>(base)[to] = x;
-      else static_cast<uint8_t*>(base)[to] = e;
-    }
-    __syncthreads();
-  }
+  const Place place = {p, int(blockIdx.z), int(blockIdx.y)};
+  auto places = [&](int i, uint32_t* to, uint32_t* from) {
+    *to = place.row(keep - recent + i);
+    *from = place.row(n - recent + i);
+  };
+  // Rows that do not overlap their new places are any block's.
+  if (n - keep >= recent) copy_moves<false, U>(p, kSelect, recent, blockIdx.x, gridDim.x, places);
+  else if (blockIdx.x == 0) copy_moves<true, U>(p, kSelect, recent, 0, 1, places);
+}
+
+// Whether one launch does it all.
+bool few_rows(int64_t keep, int64_t recent, int64_t max_length) {
+  return max_length <= keep || (max_length <= kFewTokens && lists_of(keep, recent, max_length).places + recent <= kFewRows);
 }
 
 template <class U>
 hipError_t launch(const KvEvictParams& p, hipStream_t stream) {
+  if (few_rows(p.keep, p.recent, p.max_length)) {
+    const size_t ranks = p.max_length <= p.keep ? 0 : size_t(p.max_length) * sizeof(uint32_t);
+    evict_few_kernel<U><<<dim3(unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), ranks, stream>>>(p);
+    return hipGetLastError();
+  }
   const Lists l = lists_of(p.keep, p.recent, p.max_length);
-  evict_select_kernel<<<dim3(unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), 0, stream>>>(p);
+  const dim3 grid(unsigned(l.chunks), unsigned(p.hk), unsigned(p.batch));
+  if (p.keep > p.recent + p.sink) {
+    evict_count_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
+    evict_bucket_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
+  }
+  evict_border_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t want = std::max((l.places + kMoveRows - 1) / kMoveRows, (p.span + 2047) / 2048);
-  const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(want, 4096 / (int64_t(p.hk) * p.batch)));
-  evict_move_kernel<U><<<dim3(unsigned(blocks), unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(p);
+  // Enough blocks for four moves a thread, or 2048 masses a block.
+  const int64_t heads = int64_t(p.hk) * p.batch;
+  auto blocks_of = [&](int64_t want) { return unsigned(std::max<int64_t>(1, std::min<int64_t>(want, std::max<int64_t>(1, 8192 / heads)))); };
+  auto moves_of = [&](int64_t moves, int threads) { return ((moves << p.row_shift) + 4 * threads - 1) / (4 * threads); };
+  const unsigned move = blocks_of(std::max(moves_of(l.places, 256), (p.span + 2047) / 2048));
+  evict_move_kernel<U><<<dim3(move, unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(p);
   e = hipGetLastError();
-  if (e != hipSuccess || p.recent == 0 || p.max_length <= p.keep) return e;
-  evict_shift_kernel<U><<<dim3(p.exp_bytes ? 4 : 2, unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(p);
+  if (e != hipSuccess || p.recent == 0) return e;
+  const unsigned shift = blocks_of(moves_of(p.recent, kSelect));
+  evict_shift_kernel<U><<<dim3(shift, unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), 0, stream>>>(p);
   return hipGetLastError();
+}
+
+// The power of two threads that have a move's 2 * units units, at most a wave.
+int shift_of(int units) {
+  int s = 1;
+  while (s < 6 && (1 << s) < 2 * units) ++s;
+  return s;
 }
 
 }  // namespace
 
 size_t evict_workspace_bytes(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length) {
+  if (few_rows(keep, recent, max_length)) return 0;
   return size_t(batch * hk * lists_of(keep, recent, max_length).stride) * sizeof(uint32_t);
 }
 
-hipError_t launch_kv_evict(const KvEvictParams& p, hipStream_t stream) {
-  if (p.row_bytes % 16 == 0) return launch<u32x4>(p, stream);
-  return launch<u32x2>(p, stream);
+hipError_t launch_kv_evict(KvEvictParams p, hipStream_t stream) {
+  const int unit = p.row_bytes % 16 == 0 ? 16 : 8;
+  p.row_shift = shift_of(p.row_bytes / unit);
+  p.exp_words = p.exp_bytes % 4 == 0 && (reinterpret_cast<uintptr_t>(p.k_exps) | reinterpret_cast<uintptr_t>(p.v_exps)) % 4 == 0;
+  p.exp_shift = shift_of(p.exp_words ? p.exp_bytes / 4 : p.exp_bytes);
+  return unit == 16 ? launch<u32x4>(p, stream) : launch<u32x2>(p, stream);
 }
 
 }  // namespace cp

@@ -350,9 +350,11 @@ struct KvEvictParams {
   int64_t keep, recent, sink;     // 1 <= keep < 2^31, 0 <= sink + recent <= keep
   int batch, hk, page, width;
   int row_bytes, exp_bytes;       // row_bytes a multiple of 8; exp_bytes 0 without exponents
+  int row_shift, exp_shift;       // these three are launch_kv_evict's
+  bool exp_words;
   void* workspace;
 };
 size_t evict_workspace_bytes(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length);
-hipError_t launch_kv_evict(const KvEvictParams& p, hipStream_t stream);
+hipError_t launch_kv_evict(KvEvictParams p, hipStream_t stream);
 
 }  // namespace cp

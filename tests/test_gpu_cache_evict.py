@@ -144,3 +144,33 @@ def test_pages_outside_the_cache_are_clamped():
     import paper_2608_13226_amd as cp
     x, y = cp.kv_evict(**a, keep=20, recent=4), cp.kv_evict(**b, keep=20, recent=4)
     assert torch.equal(x.kept, y.kept) and torch.equal(_raw(a["v_cache"]), _raw(b["v_cache"]))
+
+
+@pytest.mark.parametrize("lengths,hk,keep,recent,sink,ties", [
+    ([20000, 16384, 2500, 16000], 2, 2500, 100, 5, False), ([40000, 39000], 2, 20000, 15000, 64, True),
+    ([16385], 1, 4000, 0, 0, True), ([30000, 12], 1, 29000, 29000, 0, False), ([30000], 2, 5000, 4000, 1000, False),
+    ([300000, 299999], 1, 150000, 100, 10, True), ([5000] * 4, 3, 2400, 300, 0, False), ([16384] * 2, 1, 8000, 8000, 0, False)])
+def test_many_rows(lengths, hk, keep, recent, sink, ties):
+    """Those that go in several launches: chunks, boundaries inside them, sequences that are short enough beside them."""
+    for held in ("e2m1", "bf16"):
+        a = _data(lengths, hk, 64, 50, held, ties=ties)
+        _check({x: y.clone() if y is not None else None for x, y in a.items()}, keep, recent, sink)
+        a["mass"][:, 0, ::7] = math.nan
+        a["mass"][:, 0, 3::11] = -math.inf
+        _check(a, keep, recent, sink, in_place=True)
+
+
+def test_all_masses_equal_in_a_long_sequence():
+    a = _data([50000], 2, 32, 64, "e2m1")
+    a["mass"].zero_()
+    _check(a, 20000, 64, 4)
+
+
+def test_exponents_without_alignment():
+    a = _data([3000, 700], 2, 128, 16, "e2m1")
+    for name in ("k_scale", "v_scale"):
+        x = a[name]
+        y = torch.empty(x.numel() + 1, dtype=torch.uint8, device="cuda")[1:].view(x.shape)
+        y.copy_(x)
+        a[name] = y
+    _check(a, 500, 50, 2)
