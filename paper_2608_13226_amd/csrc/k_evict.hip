@@ -13,7 +13,7 @@
 // from counts as well, so nothing depends on the order of atomics.
 //
 //   evict_few    where few rows move, all of it by a block a (sequence, head), the
-//                ranks in LDS
+//                masses in LDS
 //   otherwise, with a sequence's tokens in up to 64 chunks:
 //   evict_count  a chunk's counts of the rank's highest 10 bits
 //   evict_bucket the value of those at which the rank wanted lies; a chunk's tokens that
@@ -54,41 +54,61 @@ __device__ __forceinline__ int lanes_below(unsigned long long ballot) {
   return int(__builtin_amdgcn_mbcnt_hi(unsigned(ballot >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(ballot), 0u)));
 }
 
-// Sum over this lane and the lower ones.
+// Sum over this lane and the lower ones; every lane of the wave is active.
 __device__ __forceinline__ int wave_upto(int x) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // from 1, 2, 4 and 8 lanes below in a row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next, rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
   return x;
 }
 
-// counts[bins * COPIES]: the digit at which the counts from the highest on reach `left`
-// (1 <= left <= their sum), and how many are left at it.  By one wave; bins a multiple of 64.
+// Counts of a digit with BINS values, COPIES each.
 template <int BINS, int COPIES>
-__device__ __forceinline__ void find_digit(const int* counts, int left, uint32_t* digit, int* rest) {
-  constexpr int kPer = BINS / kWave;
-  const int lane = threadIdx.x % kWave, top = BINS - 1 - lane * kPer;
-  int sum = 0;
-#pragma unroll 4
-  for (int i = 0; i < kPer * COPIES; ++i) sum += counts[(top - kPer + 1) * COPIES + i];
-  const int upto = wave_upto(sum);
-  int before = upto - sum;
-  if (before < left && left <= upto) {
-    for (int i = 0; i < kPer; ++i) {
-      int c = 0;
-      for (int e = 0; e < COPIES; ++e) c += counts[(top - i) * COPIES + e];
-      if (left <= before + c) {
-        *digit = uint32_t(top - i);
-        *rest = left - before;
-        break;
-      }
-      before += c;
-    }
+struct Digits {
+  static constexpr int kPer = BINS / kSelect;
+  int count[BINS * COPIES], upto[kWaves], left;
+  uint32_t digit;
+
+  __device__ __forceinline__ void clear() {
+    for (int i = threadIdx.x; i < BINS * COPIES; i += kSelect) count[i] = 0;
   }
-}
+  __device__ __forceinline__ void add(uint32_t d) { atomicAdd(&count[d * COPIES + threadIdx.x % COPIES], 1); }
+
+  // The digit at which the counts from the highest on reach `rest` (1 <= rest <= their
+  // sum), and how many are left at it.  The block has synchronised after its last add.
+  __device__ __forceinline__ uint32_t find(int& rest) {
+    const int wave = threadIdx.x / kWave, top = BINS - 1 - int(threadIdx.x) * kPer;
+    int c[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      c[i] = 0;
+#pragma unroll
+      for (int e = 0; e < COPIES; ++e) c[i] += count[(top - i) * COPIES + e];
+      sum += c[i];
+    }
+    const int here = wave_upto(sum);
+    if (threadIdx.x % kWave == kWave - 1) upto[wave] = here;
+    lds_sync();
+    int before = here - sum;
+    for (int w = 0; w < wave; ++w) before += upto[w];
+    if (before < rest && rest <= before + sum) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (before < rest && rest <= before + c[i]) {
+          digit = uint32_t(top - i);
+          left = rest - before;
+        }
+        before += c[i];
+      }
+    }
+    lds_sync();
+    rest = left;
+    return digit;
+  }
+};
 
 // Rows of a sequence and head.
 struct Place {
@@ -102,14 +122,16 @@ struct Place {
   }
 };
 
-// Moves first, first + step, ... of `moves` rows from one place to another by a block of
-// `threads`: 2^shift threads have a key's `units` units, then a value's, and four moves
-// at a time.  places(move, to, from) gives the rows.  IN_ORDER: rows may overlap their
-// new places; a lower move's row is read before a higher one's is written.
-template <bool IN_ORDER, class X, class Places>
-__device__ __forceinline__ void copy_rows(X* keys, X* values, int units, int shift, int threads, int moves, int first, int step, Places places) {
-  const int lanes = 1 << shift, u0 = int(threadIdx.x) & (lanes - 1), per = threads >> shift;
-  const int mine = int(threadIdx.x) >> shift;
+// Batches first, first + step, ... of `moves` rows from one place to another by a block
+// of `threads`: 2^row_shift threads have a key's units, then a value's (and a part of
+// either's exponents), four moves at a time.  places(move, to, from) gives the rows.
+// IN_ORDER: rows may overlap their new places; a lower move's row is read before a
+// higher one's is written, and all threads come along.
+template <bool IN_ORDER, class U, class E, class Places>
+__device__ __forceinline__ void copy_rows(const KvEvictParams& p, E* k_exps, E* v_exps, int exp_units, int threads, int moves, int first,
+                                          int step, Places places) {
+  const int units = p.row_bytes / int(sizeof(U)), lanes = 1 << p.row_shift, u0 = int(threadIdx.x) & (lanes - 1);
+  const int per = threads >> p.row_shift, mine = int(threadIdx.x) >> p.row_shift;
   for (int64_t i0 = int64_t(first) * 4 * per; i0 < moves; i0 += int64_t(step) * 4 * per) {
     uint32_t to[4], from[4];
 #pragma unroll
@@ -117,51 +139,55 @@ __device__ __forceinline__ void copy_rows(X* keys, X* values, int units, int shi
       const int64_t i = i0 + e * per + mine;
       if (i < moves) places(int(i), &to[e], &from[e]);
     }
-    // (One turn but for rows of over 64 units.)
+    // (One turn but for rows of over 32 units.)
     for (int u = u0; IN_ORDER ? u - u0 < 2 * units : u < 2 * units; u += lanes) {
-      X* base = u < units ? keys : values;
+      U* rows = static_cast<U*>(u < units ? p.k_cache : p.v_cache);
+      E* exps = u < units ? k_exps : v_exps;
       const int v = u < units ? u : u - units;
-      X x[4];
+      U x[4];
+      E y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (u < 2 * units && i0 + e * per + mine < moves) x[e] = base[int64_t(from[e]) * units + v];
+        if (u < 2 * units && i0 + e * per + mine < moves) {
+          x[e] = rows[int64_t(from[e]) * units + v];
+          if (v < exp_units) y[e] = exps[int64_t(from[e]) * exp_units + v];
+        }
       if (IN_ORDER) __syncthreads();
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (u < 2 * units && i0 + e * per + mine < moves) base[int64_t(to[e]) * units + v] = x[e];
+        if (u < 2 * units && i0 + e * per + mine < moves) {
+          rows[int64_t(to[e]) * units + v] = x[e];
+          if (v < exp_units) exps[int64_t(to[e]) * exp_units + v] = y[e];
+        }
       if (IN_ORDER) __syncthreads();
     }
   }
 }
-
-// All of them: keys, values and exponents.
+// (The units of exponents are at most as many as a row's: d / 32 bytes or fewer words, and d / 32 units of 16 bytes.)
 template <bool IN_ORDER, class U, class Places>
 __device__ __forceinline__ void copy_moves(const KvEvictParams& p, int threads, int moves, int first, int step, Places places) {
-  copy_rows<IN_ORDER>(static_cast<U*>(p.k_cache), static_cast<U*>(p.v_cache), p.row_bytes / int(sizeof(U)), p.row_shift, threads, moves,
-                      first, step, places);
-  if (p.exp_bytes == 0) return;
   if (p.exp_words)
-    copy_rows<IN_ORDER>(reinterpret_cast<uint32_t*>(p.k_exps), reinterpret_cast<uint32_t*>(p.v_exps), p.exp_bytes / 4, p.exp_shift,
-                        threads, moves, first, step, places);
+    copy_rows<IN_ORDER, U>(p, reinterpret_cast<uint32_t*>(p.k_exps), reinterpret_cast<uint32_t*>(p.v_exps), p.exp_bytes / 4, threads,
+                           moves, first, step, places);
   else
-    copy_rows<IN_ORDER>(p.k_exps, p.v_exps, p.exp_bytes, p.exp_shift, threads, moves, first, step, places);
+    copy_rows<IN_ORDER, U>(p, p.k_exps, p.v_exps, p.exp_bytes, threads, moves, first, step, places);
 }
 
 // ---------------------------------------------------------------------------
 // Few rows: one launch.
 
-constexpr int kFewTokens = 16384;   // whose ranks are in LDS
+constexpr int kFewTokens = 16384;   // whose masses are in LDS
 constexpr int kFewRows = 2048;      // that move: vacant places and `recent`
-constexpr int kCopies = 8;          // of each count: most masses share their highest bits, and
-                                    // additions to one address wait for each other
+using Top = Digits<4096, 2>;        // of the rank's highest 12 bits: most masses share an octave or two, and
+using Low = Digits<1024, 1>;        // additions to one address wait for each other; then two digits of 10
 
 template <class U>
 __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
-  extern __shared__ uint32_t s_rank[];                      // [max_length]
-  __shared__ int s_hist[2][256 * kCopies];
+  extern __shared__ float s_mass[];                         // [max_length]
+  __shared__ Top s_top;
+  __shared__ Low s_low[2];
   __shared__ uint32_t s_to[kFewRows], s_from[kFewRows];     // tokens, then their rows
-  __shared__ uint32_t s_digit;
-  __shared__ int s_left, s_ties[kWaves], s_both[kWaves];
+  __shared__ int s_ties[kWaves], s_both[kWaves];
   const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink), m = min(n, keep);
   const int64_t head = int64_t(b) * p.hk + kh;
@@ -175,34 +201,36 @@ __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
     return;
   }
   const int end = n - recent, front = keep - recent, want = front - sink;
-  for (int i = tid; i < 2 * 256 * kCopies; i += kSelect) s_hist[0][i] = 0;
-#pragma unroll 4
-  for (int j = tid; j < end; j += kSelect) s_rank[j] = rank_of(mass[j]);
+  s_top.clear();
+  s_low[0].clear();
+  s_low[1].clear();
+#pragma unroll 16
+  for (int j = tid; j < n; j += kSelect) s_mass[j] = mass[j];
   lds_sync();
   uint32_t border = 0u;
   int ties = want;
   if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      int* hist = s_hist[shift / 8 % 2];
+#pragma unroll 4
+    for (int j = sink + tid; j < end; j += kSelect) s_top.add(rank_of(s_mass[j]) >> 20);
+    lds_sync();
+    border = s_top.find(ties) << 20;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int shift = 10 - 10 * i;
 #pragma unroll 4
       for (int j = sink + tid; j < end; j += kSelect) {
-        const uint32_t r = s_rank[j];
-        // (In two steps, so that nothing is left of them the first time.)
-        if ((r ^ border) >> shift >> 8 == 0u) atomicAdd(&hist[(r >> shift & 255u) * kCopies + lane % kCopies], 1);
+        const uint32_t r = rank_of(s_mass[j]);
+        if ((r ^ border) >> (shift + 10) == 0u) s_low[i].add(r >> shift & 1023u);
       }
       lds_sync();
-      if (wave == 0) find_digit<256, kCopies>(hist, ties, &s_digit, &s_left);
-      lds_sync();
-      border |= s_digit << shift;
-      ties = s_left;
-      for (int i = tid; i < 256 * kCopies; i += kSelect) hist[i] = 0;
+      border |= s_low[i].find(ties) << shift;
     }
   }
   // Each wave has consecutive tokens: how many are at the border, then how many places
   // fall vacant below the front and how many tokens from it on stay.
   const int run = (end + kSelect - 1) / kSelect * kWave, j0 = wave * run, j1 = min(end, j0 + run);
   int equal = 0;
-  for (int j = j0 + lane; j < j1; j += kWave) equal += __popcll(__ballot(want > 0 && j >= sink && s_rank[j] == border));
+  for (int j = j0 + lane; j < j1; j += kWave) equal += __popcll(__ballot(want > 0 && j >= sink && rank_of(s_mass[j]) == border));
   if (lane == 0) s_ties[wave] = j0 < j1 ? equal : 0;
   lds_sync();
   int tie0 = 0;
@@ -210,7 +238,7 @@ __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
   // Token j (every lane of the wave comes along): whether it stays; `seen` counts ties.
   auto stays = [&](int j, int& seen) {
     const bool here = j < j1;
-    const uint32_t r = here ? s_rank[j] : 0u;
+    const uint32_t r = here ? rank_of(s_mass[j]) : 0u;
     const bool tie = here && want > 0 && j >= sink && r == border;
     const unsigned long long all = __ballot(tie);
     const bool yes = here && (j < sink || (want > 0 && (r > border || (tie && seen + lanes_below(all) < ties))));
@@ -241,7 +269,7 @@ __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
     const unsigned long long all_gaps = __ballot(gap), all_go = __ballot(go);
     if (yes && !go) {
       kept[j] = j;
-      if (out != mass) out[j] = mass[j];
+      out[j] = s_mass[j];
     }
     if (gap) s_to[gap_at + lanes_below(all_gaps)] = j;
     if (go) s_from[go_at + lanes_below(all_go)] = j;
@@ -254,20 +282,15 @@ __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
     s_from[i] = end + i - total;
   }
   lds_sync();
-  // The masses like the rows: first those that go below the front, then the last ones in
-  // ascending runs, each read whole before it is written.
-  for (int i = tid; i < moves; i += kSelect) kept[s_to[i]] = s_from[i];
-  for (int i = tid; i < total; i += kSelect) out[s_to[i]] = mass[s_from[i]];
-  for (int i0 = total; i0 < moves; i0 += kSelect) {
-    const int i = i0 + tid;
-    const float v = i < moves ? mass[s_from[i]] : 0.f;
-    __syncthreads();
-    if (i < moves) out[s_to[i]] = v;
+  for (int i = tid; i < moves; i += kSelect) {
+    const int to = s_to[i], from = s_from[i];
+    kept[to] = from;
+    out[to] = s_mass[from];
   }
-  __syncthreads();
   for (int64_t j = m + tid; j < p.span; j += kSelect) out[j] = 0.f;
   const Place place = {p, b, kh};
   for (int i = tid; i < moves; i += kSelect) {
+    // (Each thread's own moves, so far.)
     s_to[i] = place.row(s_to[i]);
     s_from[i] = place.row(s_from[i]);
   }
@@ -343,46 +366,58 @@ struct Chunk {
     w0 = min(j1, j0 + int(threadIdx.x) / kWave * per);
     w1 = min(j1, w0 + per);
   }
+
+  // f(token, whether it is one, its mass) for this wave's tokens in order, 64 at a time and all
+  // lanes together; four loads are under way at once.
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    const int lane = threadIdx.x % kWave;
+    for (int t = w0; t < w1; t += 4 * kWave) {
+      float m[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = t + e * kWave + lane < w1 ? mass[t + e * kWave + lane] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (t + e * kWave < w1) f(t + e * kWave + lane, t + e * kWave + lane < w1, m[e]);
+    }
+  }
 };
 
 __global__ __launch_bounds__(kSelect) void evict_count_kernel(KvEvictParams p) {
-  __shared__ int s_hist[kBuckets * 4];
+  __shared__ Digits<kBuckets, 2> s_top;
   const Chunk c(p);
   const int tid = threadIdx.x;
   if (c.end == 0) return;
-  for (int i = tid; i < kBuckets * 4; i += kSelect) s_hist[i] = 0;
+  s_top.clear();
   lds_sync();
-#pragma unroll 4
-  for (int j = max(c.j0, c.sink) + tid; j < c.j1; j += kSelect) atomicAdd(&s_hist[(rank_of(c.mass[j]) >> 22) * 4 + tid % 4], 1);
+  c.each([&](int j, bool here, float m) {
+    if (here && j >= c.sink) s_top.add(rank_of(m) >> 22);
+  });
   lds_sync();
-  c.ws[c.l.hist + int64_t(blockIdx.x) * kBuckets + tid] = s_hist[tid * 4] + s_hist[tid * 4 + 1] + s_hist[tid * 4 + 2] + s_hist[tid * 4 + 3];
+  c.ws[c.l.hist + int64_t(blockIdx.x) * kBuckets + tid] = uint32_t(s_top.count[2 * tid] + s_top.count[2 * tid + 1]);
 }
 
 __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) {
-  __shared__ int s_hist[kBuckets];
+  __shared__ Digits<kBuckets, 1> s_top;
   __shared__ int s_part[3][kWaves];
-  __shared__ uint32_t s_digit;
-  __shared__ int s_left;
   const Chunk c(p);
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   if (c.end == 0 || c.want == 0) return;
   int sum = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (int i = 0; i < c.l.chunks; ++i) sum += int(c.ws[c.l.hist + int64_t(i) * kBuckets + tid]);
-  s_hist[tid] = sum;
+  s_top.count[tid] = sum;
   lds_sync();
-  if (wave == 0) find_digit<kBuckets, 1>(s_hist, c.want, &s_digit, &s_left);
-  lds_sync();
-  const uint32_t bucket = s_digit;
+  int ties = c.want;
+  const uint32_t bucket = s_top.find(ties);
   int in = 0, low = 0, high = 0;
-  for (int t = c.w0; t < c.w1; t += kWave) {
-    const int j = t + lane;
-    const bool here = j < c.w1 && j >= c.sink;
-    const uint32_t top = here ? rank_of(c.mass[j]) >> 22 : 0u;
+  c.each([&](int j, bool here, float m) {
+    here = here && j >= c.sink;
+    const uint32_t top = rank_of(m) >> 22;
     in += __popcll(__ballot(here && top == bucket));
     low += __popcll(__ballot(here && top > bucket && j < c.front));
     high += __popcll(__ballot(here && top > bucket && j >= c.front));
-  }
+  });
   if (lane == 0) {
     s_part[0][wave] = in;
     s_part[1][wave] = low;
@@ -392,16 +427,14 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
   int at = 0;
   for (int w = 0; w < wave; ++w) at += s_part[0][w];
   uint32_t* some = c.ws + c.l.some + c.j0;
-  for (int t = c.w0; t < c.w1; t += kWave) {
-    const int j = t + lane;
-    const bool here = j < c.w1 && j >= c.sink;
-    const uint32_t r = here ? rank_of(c.mass[j]) : 0u;
-    const bool yes = here && r >> 22 == bucket;
+  c.each([&](int j, bool here, float m) {
+    const uint32_t r = rank_of(m);
+    const bool yes = here && j >= c.sink && r >> 22 == bucket;
     const unsigned long long all = __ballot(yes);
     // The rank's other 22 bits, and whether it is below the front.
     if (yes) some[at + lanes_below(all)] = (r & 0x3fffffu) | uint32_t(j < c.front) << 31;
     at += __popcll(all);
-  }
+  });
   if (tid < 4) {
     int x = int(bucket);
     if (tid < 3) {
@@ -411,15 +444,13 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
     c.ws[c.l.stats + int64_t(blockIdx.x) * 4 + tid] = uint32_t(x);
   }
   // (Every block finds the same; the first leaves it.)
-  if (blockIdx.x == 0 && tid == 0) c.ws[c.l.ties] = uint32_t(s_left);
+  if (blockIdx.x == 0 && tid == 0) c.ws[c.l.ties] = uint32_t(ties);
 }
 
 __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) {
-  __shared__ int s_hist[2048 * 4];
-  __shared__ uint32_t s_digit;
-  __shared__ int s_left;
+  __shared__ Digits<2048, 2> s_low_digits;
   __shared__ int s_equal[64], s_low[64], s_high[64], s_equal_low[64];
-  __shared__ int s_part[kWaves], s_both[2][kWaves];
+  __shared__ int s_wave[4][kWaves];
   const Chunk c(p);
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   int32_t* kept = p.kept + c.head * p.keep;
@@ -441,7 +472,7 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     uint32_t low = 0u;
 #pragma unroll 1
     for (int shift = kRest; shift >= 0; shift -= kRest) {
-      for (int i = tid; i < 2048 * 4; i += kSelect) s_hist[i] = 0;
+      s_low_digits.clear();
       lds_sync();
       // A wave takes every 16th chunk's tokens of the bucket.
       for (int k = wave; k < c.l.chunks; k += kWaves) {
@@ -450,14 +481,11 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
 #pragma unroll 4
         for (int i = lane; i < count; i += kWave) {
           const uint32_t r = some[i] & 0x3fffffu;
-          if (shift == kRest || r >> kRest == low >> kRest) atomicAdd(&s_hist[(r >> shift & 2047u) * 4 + lane % 4], 1);
+          if (shift == kRest || r >> kRest == low >> kRest) s_low_digits.add(r >> shift & 2047u);
         }
       }
       lds_sync();
-      if (wave == 0) find_digit<2048, 4>(s_hist, ties, &s_digit, &s_left);
-      lds_sync();
-      low |= s_digit << shift;
-      ties = s_left;
+      low |= s_low_digits.find(ties) << shift;
     }
     border = bucket << 22 | low;
     // Each chunk's tokens at the border and above it.
@@ -485,65 +513,54 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     s_equal[tid] = s_equal_low[tid] = s_low[tid] = s_high[tid] = 0;
   }
   lds_sync();
-  // Up to this chunk: ties, vacant places, movers.  And all vacant places.
-  int tie0 = 0, gap0 = 0, go0 = 0, gaps = 0;
+  // Up to this chunk: ties, vacant places, movers.  And all vacant places.  Lane k has chunk k.
+  int tie0, gap0, go0, gaps;
   {
-    int seen = 0;
-    for (int k = 0; k < c.l.chunks; ++k) {
-      const int a = k * c.l.chunk, z = min(c.front, min(c.end, a + c.l.chunk));
-      const int taken = min(max(ties - seen, 0), s_equal[k]), taken_low = min(taken, s_equal_low[k]);
-      const int sinks = min(max(c.sink - a, 0), c.l.chunk);
-      if (k < int(blockIdx.x)) {
-        tie0 += s_equal[k];
-        go0 += s_high[k] + taken - taken_low;
-      }
-      gaps += max(z - a, 0) - (sinks + s_low[k] + taken_low);
-      if (k < int(blockIdx.x)) gap0 = gaps;
-      seen += s_equal[k];
-    }
+    const int k = min(lane, c.l.chunks - 1), a = k * c.l.chunk, z = min(c.front, min(c.end, a + c.l.chunk));
+    const int equal = lane < c.l.chunks ? s_equal[k] : 0, before = wave_upto(equal) - equal;
+    const int taken = min(max(ties - before, 0), equal), taken_low = min(taken, s_equal_low[k]);
+    const int sinks = min(max(c.sink - a, 0), c.l.chunk);
+    const int gap = lane < c.l.chunks ? max(z - a, 0) - (sinks + s_low[k] + taken_low) : 0, go = s_high[k] + taken - taken_low;
+    const int gaps_upto = wave_upto(gap), go_upto = wave_upto(go), me = int(blockIdx.x);
+    tie0 = __builtin_amdgcn_readlane(before, me);
+    gap0 = __builtin_amdgcn_readlane(gaps_upto - gap, me);
+    go0 = __builtin_amdgcn_readlane(go_upto - go, me);
+    gaps = __builtin_amdgcn_readlane(gaps_upto, kWave - 1);
   }
-  auto rank = [&](int j) { return rank_of(c.mass[j]); };
-  int equal = 0;
-  for (int t = c.w0; t < c.w1; t += kWave) {
-    const int j = t + lane;
-    equal += __popcll(__ballot(j < c.w1 && c.want > 0 && j >= c.sink && rank(j) == border));
-  }
-  if (lane == 0) s_part[wave] = equal;
-  lds_sync();
-  for (int w = 0; w < wave; ++w) tie0 += s_part[w];
-  auto stays = [&](int j, float m, int& seen) {
-    const bool here = j < c.w1;
+  // Then up to this wave, from each wave's tokens at the border and above it.
+  int equal = 0, equal_low = 0, above_low = 0, above_high = 0;
+  c.each([&](int j, bool here, float m) {
     const uint32_t r = rank_of(m);
-    const bool tie = here && c.want > 0 && j >= c.sink && r == border;
-    const unsigned long long all = __ballot(tie);
-    const bool yes = here && (j < c.sink || (c.want > 0 && (r > border || (tie && seen + lanes_below(all) < ties))));
-    seen += __popcll(all);
-    return yes;
-  };
-  int seen = tie0, my_gaps = 0, my_go = 0;
-  for (int t = c.w0; t < c.w1; t += kWave) {
-    const int j = t + lane;
-    const bool yes = stays(j, j < c.w1 ? c.mass[j] : 0.f, seen);
-    my_gaps += __popcll(__ballot(j < c.w1 && !yes && j < c.front));
-    my_go += __popcll(__ballot(yes && j >= c.front));
-  }
+    const bool inner = here && c.want > 0 && j >= c.sink, above = here && (j < c.sink || (inner && r > border));
+    equal += __popcll(__ballot(inner && r == border));
+    equal_low += __popcll(__ballot(inner && r == border && j < c.front));
+    above_low += __popcll(__ballot(above && j < c.front));
+    above_high += __popcll(__ballot(above && j >= c.front));
+  });
   if (lane == 0) {
-    s_both[0][wave] = my_gaps;
-    s_both[1][wave] = my_go;
+    s_wave[0][wave] = equal;
+    s_wave[1][wave] = equal_low;
+    s_wave[2][wave] = above_low;
+    s_wave[3][wave] = above_high;
   }
   lds_sync();
   for (int w = 0; w < wave; ++w) {
-    gap0 += s_both[0][w];
-    go0 += s_both[1][w];
+    const int a = min(c.j1, c.j0 + w * c.per), z = max(a, min(c.front, min(c.j1, a + c.per)));
+    const int taken = min(max(ties - tie0, 0), s_wave[0][w]), taken_low = min(taken, s_wave[1][w]);
+    tie0 += s_wave[0][w];
+    gap0 += z - a - s_wave[2][w] - taken_low;
+    go0 += s_wave[3][w] + taken - taken_low;
   }
   int *vacant = reinterpret_cast<int*>(c.ws + c.l.vacant), *movers = reinterpret_cast<int*>(c.ws + c.l.movers);
   float* mover_mass = reinterpret_cast<float*>(c.ws + c.l.mover_mass);
-  seen = tie0;
-  for (int t = c.w0; t < c.w1; t += kWave) {
-    const int j = t + lane;
-    const float m = j < c.w1 ? c.mass[j] : 0.f;
-    const bool yes = stays(j, m, seen), gap = j < c.w1 && !yes && j < c.front, go = yes && j >= c.front;
+  c.each([&](int j, bool here, float m) {
+    const uint32_t r = rank_of(m);
+    const bool inner = here && c.want > 0 && j >= c.sink, tie = inner && r == border;
+    const unsigned long long all_ties = __ballot(tie);
+    const bool yes = here && (j < c.sink || (inner && r > border) || (tie && tie0 + lanes_below(all_ties) < ties));
+    const bool gap = here && !yes && j < c.front, go = yes && j >= c.front;
     const unsigned long long all_gaps = __ballot(gap), all_go = __ballot(go);
+    tie0 += __popcll(all_ties);
     if (yes && !go) {
       kept[j] = j;
       fresh[j] = m;
@@ -559,7 +576,7 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     }
     gap0 += __popcll(all_gaps);
     go0 += __popcll(all_go);
-  }
+  });
   for (int i = int(blockIdx.x) * kSelect + tid; i < p.recent; i += int(gridDim.x) * kSelect) {
     kept[c.front + i] = c.end + i;
     fresh[c.front + i] = c.mass[c.end + i];
@@ -568,7 +585,7 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
 }
 
 template <class U>
-__global__ __launch_bounds__(256) void evict_move_kernel(KvEvictParams p) {
+__global__ __launch_bounds__(256) void evict_move_kernel(KvEvictParams p, int mass_blocks) {
   const int kh = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int64_t head = int64_t(b) * p.hk + kh;
   const Lists l = lists_of(p.keep, p.recent, p.max_length);
@@ -579,18 +596,24 @@ __global__ __launch_bounds__(256) void evict_move_kernel(KvEvictParams p) {
   float* mass = p.mass_out + head * p.span;
   int32_t* kept = p.kept + head * p.keep;
   const int front = n > m ? int(p.keep - p.recent) : m;
-  const int first = int(blockIdx.x) * 256 + tid, step = int(gridDim.x) * 256;
-  for (int64_t j = first; j < p.span; j += step) {
-    // A vacant place's mass comes below.
-    if (j >= front || kept[j] == j) mass[j] = j < m ? fresh[j] : 0.f;
+  // The first blocks have the masses, the others the rows.
+  if (int(blockIdx.x) < mass_blocks) {
+    const int first = int(blockIdx.x) * 256 + tid, step = mass_blocks * 256;
+#pragma unroll 4
+    for (int64_t j = first; j < p.span; j += step) {
+      // A vacant place's mass comes below.
+      if (j >= front || kept[j] == j) mass[j] = j < m ? fresh[j] : 0.f;
+    }
+#pragma unroll 2
+    for (int i = first; i < gaps; i += step) {
+      mass[vacant[i]] = mover_mass[i];
+      kept[vacant[i]] = movers[i];
+    }
+    if (kh == 0 && first == 0) p.lengths_out[b] = m;
+    return;
   }
-  for (int i = first; i < gaps; i += step) {
-    mass[vacant[i]] = mover_mass[i];
-    kept[vacant[i]] = movers[i];
-  }
-  if (kh == 0 && first == 0) p.lengths_out[b] = m;
   const Place place = {p, b, kh};
-  copy_moves<false, U>(p, 256, gaps, blockIdx.x, gridDim.x, [&](int i, uint32_t* to, uint32_t* from) {
+  copy_moves<false, U>(p, 256, gaps, int(blockIdx.x) - mass_blocks, int(gridDim.x) - mass_blocks, [&](int i, uint32_t* to, uint32_t* from) {
     *to = place.row(vacant[i]);
     *from = place.row(movers[i]);
   });
@@ -635,8 +658,8 @@ hipError_t launch(const KvEvictParams& p, hipStream_t stream) {
   const int64_t heads = int64_t(p.hk) * p.batch;
   auto blocks_of = [&](int64_t want) { return unsigned(std::max<int64_t>(1, std::min<int64_t>(want, std::max<int64_t>(1, 8192 / heads)))); };
   auto moves_of = [&](int64_t moves, int threads) { return ((moves << p.row_shift) + 4 * threads - 1) / (4 * threads); };
-  const unsigned move = blocks_of(std::max(moves_of(l.places, 256), (p.span + 2047) / 2048));
-  evict_move_kernel<U><<<dim3(move, unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(p);
+  const unsigned masses = blocks_of((p.span + 2047) / 2048), move = masses + (l.places ? blocks_of(moves_of(l.places, 256)) : 0u);
+  evict_move_kernel<U><<<dim3(move, unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(p, int(masses));
   e = hipGetLastError();
   if (e != hipSuccess || p.recent == 0) return e;
   const unsigned shift = blocks_of(moves_of(p.recent, kSelect));
@@ -662,7 +685,6 @@ hipError_t launch_kv_evict(KvEvictParams p, hipStream_t stream) {
   const int unit = p.row_bytes % 16 == 0 ? 16 : 8;
   p.row_shift = shift_of(p.row_bytes / unit);
   p.exp_words = p.exp_bytes % 4 == 0 && (reinterpret_cast<uintptr_t>(p.k_exps) | reinterpret_cast<uintptr_t>(p.v_exps)) % 4 == 0;
-  p.exp_shift = shift_of(p.exp_words ? p.exp_bytes / 4 : p.exp_bytes);
   return unit == 16 ? launch<u32x4>(p, stream) : launch<u32x2>(p, stream);
 }
 

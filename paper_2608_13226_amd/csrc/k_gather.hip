@@ -10,39 +10,54 @@
 namespace cp {
 namespace {
 
-// VEC = 8 needs d % 8 == 0; VEC = 1 is for the rest.  A token's 2 hk heads have runs = d / VEC each.
+// VEC = 8 needs d % 8 == 0; VEC = 1 is for the rest.  A token's 2 hk heads have runs =
+// d / VEC each; a thread takes kAhead runs, 256 apart, so that its loads are under way together.
+constexpr int kAhead = 4;
+
 template <class T, int BITS, int VEC>
-__global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, int64_t first_block) {
-  const int64_t runs = p.d / VEC, a_token = 2 * int64_t(p.hk) * runs;
-  const int64_t w = (first_block + blockIdx.x) * 256 + threadIdx.x;
-  const int64_t token = w / a_token;
-  if (token >= p.tokens) return;
-  int64_t r = w - token * a_token;
-  const bool is_v = r >= int64_t(p.hk) * runs;
-  if (is_v) r -= int64_t(p.hk) * runs;
-  const int kh = int(r / runs), e = int(r - kh * runs) * VEC;
-  const int64_t slot = p.slots[token], to = (token * p.hk + kh) * p.d + e;
-  void* out = is_v ? p.v_out : p.k_out;
-  if (slot < 0 || slot >= p.pages * p.page) {
-    if constexpr (VEC == 8) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) = u32x4{0, 0, 0, 0};
-    else static_cast<uint16_t*>(out)[to] = 0;
-    return;
+struct Run {
+  static constexpr int kWords = VEC == 1 ? 1 : BITS / 4;
+  uint32_t w[kWords];
+  float scale;
+
+  __device__ __forceinline__ void load(const KvGatherParams& p, bool is_v, int64_t row, int kh, int e) {
+    const uint8_t* cache = static_cast<const uint8_t*>(is_v ? p.v_cache : p.k_cache);
+    const void* scales = is_v ? p.v_scale : p.k_scale;
+    if constexpr (BITS == 16) {
+      const uint16_t* x = reinterpret_cast<const uint16_t*>(cache) + row * p.d + e;
+      if constexpr (VEC == 1) {
+        w[0] = *x;
+      } else {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = v[i];
+      }
+    } else if constexpr (BITS == 8) {
+      const uint8_t* x = cache + row * p.d + e;
+      if constexpr (VEC == 1) {
+        w[0] = *x;
+      } else {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(x);
+        w[0] = v[0];
+        w[1] = v[1];
+      }
+      scale = scales ? static_cast<const float*>(scales)[kh] : 1.f;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(cache + row * (p.d / 2) + e / 2);
+      scale = power_of(static_cast<const uint8_t*>(scales)[row * (p.d / kBlock4) + e / kBlock4]);
+    }
   }
-  const int64_t pg = slot / p.page, row = (pg * p.hk + kh) * p.page + (slot - pg * p.page);
-  const uint8_t* cache = static_cast<const uint8_t*>(is_v ? p.v_cache : p.k_cache);
-  if constexpr (BITS == 16) {
-    if constexpr (VEC == 8)
-      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) = *reinterpret_cast<const u32x4*>(cache + (row * p.d + e) * 2);
-    else static_cast<uint16_t*>(out)[to] = reinterpret_cast<const uint16_t*>(cache)[row * p.d + e];
-  } else if constexpr (BITS == 8) {
-    const float* scales = static_cast<const float*>(is_v ? p.v_scale : p.k_scale);
-    const float scale = scales ? scales[kh] : 1.f;
-    if constexpr (VEC == 8) {
-      const u32x2 v = *reinterpret_cast<const u32x2*>(cache + row * p.d + e);
+  __device__ __forceinline__ void store(void* out, int64_t to) const {
+    if constexpr (VEC == 1) {
+      if constexpr (BITS == 16) static_cast<uint16_t*>(out)[to] = uint16_t(w[0]);
+      else store1<T>(out, to, unpack2<Bf16>(widen2<Bf16, false>(w[0])).x * scale);
+    } else if constexpr (BITS == 16) {
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) = u32x4{w[0], w[1], w[2], w[3]};
+    } else if constexpr (BITS == 8) {
       float x[8];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float2 lo = unpack2<Bf16>(widen2<Bf16, false>(v[i])), hi = unpack2<Bf16>(widen2<Bf16, true>(v[i]));
+        const float2 lo = unpack2<Bf16>(widen2<Bf16, false>(w[i])), hi = unpack2<Bf16>(widen2<Bf16, true>(w[i]));
         x[4 * i] = lo.x * scale;
         x[4 * i + 1] = lo.y * scale;
         x[4 * i + 2] = hi.x * scale;
@@ -50,21 +65,50 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, int64_
       }
       store8<T>(out, to, x);
     } else {
-      store1<T>(out, to, unpack2<Bf16>(widen2<Bf16, false>(cache[row * p.d + e])).x * scale);
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) =
+          u32x4{open2<T>(w[0], scale, 0), open2<T>(w[0], scale, 1), open2<T>(w[0], scale, 2), open2<T>(w[0], scale, 3)};
     }
-  } else {
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(cache + row * (p.d / 2) + e / 2);
-    const uint8_t* exps = static_cast<const uint8_t*>(is_v ? p.v_scale : p.k_scale);
-    const float s = power_of(exps[row * (p.d / kBlock4) + e / kBlock4]);
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + to) = u32x4{open2<T>(v, s, 0), open2<T>(v, s, 1), open2<T>(v, s, 2), open2<T>(v, s, 3)};
+  }
+};
+
+// `tokens` tokens a block: a_token = 2 hk runs of them each, so that a run's token comes from a 32-bit division.
+template <class T, int BITS, int VEC>
+__global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, int tokens, int64_t first_block) {
+  const unsigned runs = unsigned(p.d / VEC), half = unsigned(p.hk) * runs, a_token = 2 * half;
+  const int64_t t0 = (first_block + blockIdx.x) * tokens;
+  const unsigned total = unsigned(min(int64_t(tokens), p.tokens - t0)) * a_token;
+  for (unsigned w0 = threadIdx.x; w0 < total; w0 += 256 * kAhead) {
+    Run<T, BITS, VEC> x[kAhead];
+    int64_t slot[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) slot[i] = p.slots[t0 + min(w0 + i * 256, total - 1) / a_token];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const unsigned w = min(w0 + i * 256, total - 1), r = w % a_token, in = r < half ? r : r - half;
+      const unsigned kh = in / runs, e = (in - kh * runs) * VEC;
+      const int64_t at = slot[i] >= 0 && slot[i] < p.pages * p.page ? slot[i] : 0;
+      // (Slots past 2^32 want a division of 64 bits.)
+      const int64_t pg = uint64_t(at) >> 32 ? at / p.page : int64_t(uint32_t(at) / uint32_t(p.page));
+      x[i].load(p, r >= half, (pg * p.hk + kh) * p.page + (at - pg * p.page), int(kh), int(e));
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const unsigned w = w0 + i * 256;
+      if (w >= total) break;
+      const unsigned token = w / a_token, r = w - token * a_token, in = r < half ? r : r - half;
+      if (slot[i] < 0 || slot[i] >= p.pages * p.page) x[i] = {};
+      x[i].store(r < half ? p.k_out : p.v_out, (t0 + token) * half * VEC + in * VEC);
+    }
   }
 }
 
 template <class T, int BITS, int VEC>
 hipError_t launch(const KvGatherParams& p, hipStream_t stream) {
-  const int64_t work = p.tokens * 2 * p.hk * (p.d / VEC);
-  return launch_blocks((work + 255) / 256, 256, [&](int64_t first, unsigned blocks) {
-    kv_gather_kernel<T, BITS, VEC><<<dim3(blocks), dim3(256), 0, stream>>>(p, first);
+  // Up to 1024 runs a block, a token's at least.
+  const int64_t a_token = 2 * int64_t(p.hk) * (p.d / VEC);
+  const int tokens = int(std::max<int64_t>(1, 256 * kAhead / a_token));
+  return launch_blocks((p.tokens + tokens - 1) / tokens, 256, [&](int64_t first, unsigned blocks) {
+    kv_gather_kernel<T, BITS, VEC><<<dim3(blocks), dim3(256), 0, stream>>>(p, tokens, first);
   });
 }
 

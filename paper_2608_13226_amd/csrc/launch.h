@@ -350,7 +350,7 @@ struct KvEvictParams {
   int64_t keep, recent, sink;     // 1 <= keep < 2^31, 0 <= sink + recent <= keep
   int batch, hk, page, width;
   int row_bytes, exp_bytes;       // row_bytes a multiple of 8; exp_bytes 0 without exponents
-  int row_shift, exp_shift;       // these three are launch_kv_evict's
+  int row_shift;                  // these two are launch_kv_evict's
   bool exp_words;
   void* workspace;
 };
