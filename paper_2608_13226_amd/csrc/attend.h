@@ -25,8 +25,9 @@
 // Caches of 4 bits are e2m1 codes with a power of two for each 32 dims: an
 // instruction widens two codes and applies the power, exactly.
 //
-// MASS: the kernel also leaves its scores, and attend_mass_kernel adds to each
-// token what its weights came to once the runs' sums are known.
+// MASS: the kernel also leaves its scores, and what each token's weights come to
+// is added to its mass once the sums of all runs are known: by the same block
+// where it has all of them, else beside the join.
 #pragma once
 
 #include <algorithm>
@@ -267,11 +268,12 @@ __device__ __forceinline__ void keep_loads_here() { asm volatile("" ::: "memory"
 // row and the lanes exchange them.
 template <class T, Held C, int D, int W, bool UNI, bool MASS>
 __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
-                                                           float* part_ml, float* scores, float* sums) {
+                                                           float* part_ml, float* scores) {
   constexpr int kSteps = D / 32;
   using L = Dims<D>;
   __shared__ float s_o[W][16][D + 4];
   __shared__ float s_m[W][16], s_l[W][16];
+  __shared__ float s_top[MASS ? 16 : 1], s_sum[MASS ? 16 : 1];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16, g = lane / 16;
   const int group = p.hq / p.hk, head_tiles = (group + 15) / 16;
@@ -462,6 +464,8 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   }
   __syncthreads();
   const float vs = p.v_scale ? p.v_scale[kh] : 1.f;
+  // Whether this block has all that there is of its heads (and, for the masses, of its key-value head).
+  const bool whole = runs == 1 && (!MASS || group <= 16);
   for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * W) {
     const int h = i / (D / 4), d = i % (D / 4) * 4;
     float M = s_m[0][h];
@@ -477,31 +481,107 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
       sum = fmaf(s_l[w][h], f, sum);
     }
     const int64_t row = int64_t(b) * p.hq + h0 + h;
-    if (runs == 1) {
+    if (whole) {
       const float k = vs / sum;
       u32x2 v;
 #pragma unroll
       for (int e = 0; e < 2; ++e) v[e] = sum == 0.f ? 0u : pack2<T>(acc[2 * e] * k, acc[2 * e + 1] * k);
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + d) = v;
       if (p.lse && d == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
-      if (MASS && d == 0) *reinterpret_cast<f32x2*>(sums + row * 2) = f32x2{M, sum};
+      if (MASS && d == 0) {
+        s_top[h] = M;
+        s_sum[h] = sum;
+      }
     } else {
       *reinterpret_cast<f32x4*>(part_o + (row * runs + run) * D + d) = acc;
       if (d == 0) *reinterpret_cast<f32x2*>(part_ml + (row * runs + run) * 2) = f32x2{M, sum};
     }
   }
+  if (!MASS || !whole) return;
+  // The scores that this block left, all of its key-value head's.
+  __syncthreads();
+  float* mass = p.mass + (int64_t(b) * p.hk + kh) * p.mass_span;
+  for (int t = lo + int(threadIdx.x); t < hi; t += 64 * W) {
+    const float* x = scores + (int64_t(b) * p.hq + h0) * (int64_t(tiles_per_run) * kTile) + (t - lo / kTile * kTile);
+    float more = 0.f;
+#pragma unroll 4
+    for (int h = 0; h < heads; ++h) {
+      const float score = x[int64_t(h) * tiles_per_run * kTile];
+      if (s_sum[h] != 0.f) more = fmaf(__builtin_amdgcn_exp2f(score - s_top[h]), 1.f / s_sum[h], more);
+    }
+    mass[t] += more;
+  }
+}
+
+// mass[b, kh, t] += sum over the heads of kh of p_t / sum_j p_j, a token a thread:
+// block `id` has THREADS consecutive ones of a (sequence, key-value head).  Its
+// waves find sixteen heads' maxima and sums from those of their runs, then all add up the heads.
+template <int THREADS>
+__device__ __forceinline__ void add_mass(const AttendParams& p, int64_t id, int runs, const float* part_ml, const float* scores,
+                                         int64_t stride) {
+  __shared__ float s_top[16], s_rec[16];
+  const int64_t chunks = (stride + THREADS - 1) / THREADS, bk = id / chunks;
+  if (bk >= int64_t(p.batch) * p.hk) return;
+  const int64_t b = bk / p.hk, at = (id - bk * chunks) * THREADS + threadIdx.x;
+  const int kh = int(bk - b * p.hk), group = p.hq / p.hk, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int hi = max(0, int(min(int64_t(p.lengths[b]), p.max_length)));
+  const int lo = p.window > 0 ? max(0, hi - p.window) : 0;
+  const int64_t t = lo / kTile * kTile + at;
+  if (t - int(threadIdx.x) >= hi) return;
+  const bool here = t >= lo && t < hi;
+  const int64_t row0 = b * p.hq + int64_t(kh) * group;
+  float* mass = p.mass + bk * p.mass_span + t;
+  const float before = here ? *mass : 0.f;
+  float more = 0.f;
+  for (int h0 = 0; h0 < group; h0 += 16) {
+    const int heads = min(16, group - h0);
+    float x[16];
+#pragma unroll
+    for (int h = 0; h < 16; ++h) x[h] = h < heads && here ? scores[(row0 + h0 + h) * stride + at] : 0.f;
+    for (int h = wave; h < heads; h += THREADS / kWave) {
+      const float2* ml = reinterpret_cast<const float2*>(part_ml) + (row0 + h0 + h) * runs;
+      float M = -INFINITY, sum = 0.f;
+      for (int s = lane; s < runs; s += kWave) {
+        const float2 v = ml[s];
+        if (v.y != 0.f) M = fmaxf(M, v.x);
+      }
+      M = wave_max(M);
+      for (int s = lane; s < runs; s += kWave) {
+        const float2 v = ml[s];
+        if (v.y != 0.f) sum = fmaf(v.y, __builtin_amdgcn_exp2f(v.x - M), sum);
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) {
+        s_top[h] = M;
+        s_rec[h] = sum == 0.f ? 0.f : 1.f / sum;      // 0: no score above -inf
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 16; ++h)
+      if (h < heads && s_rec[h] != 0.f) more = fmaf(__builtin_amdgcn_exp2f(x[h] - s_top[h]), s_rec[h], more);
+    if (h0 + 16 < group) __syncthreads();
+  }
+  if (here) *mass = before + more;
 }
 
 // The runs of one (sequence, query head) joined, DIMS dims a block.  The runs'
 // weights are found once, in LDS; then DIMS / 4 threads read their part of a
 // run and the block's other threads those of others, four runs under way each.
-template <class T, int DIMS, int kJoinThreads>
+template <class T, int DIMS, int kJoinThreads, bool MASS>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams p, int runs, const float* part_o,
-                                                                   const float* part_ml, float* sums) {
+                                                                   const float* part_ml, const float* scores, int64_t stride) {
   constexpr int kLanes = DIMS / 4, kRows = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave;
   extern __shared__ float s_f[];                // [runs] weights
   __shared__ float s_red[2][kWaves];
   __shared__ f32x4 s_acc[kRows][kLanes];
+  if constexpr (MASS) {
+    const int64_t rows = int64_t(p.batch) * p.hq;
+    if (blockIdx.x >= rows) {
+      add_mass<kJoinThreads>(p, (blockIdx.x - rows) * gridDim.y + blockIdx.y, runs, part_ml, scores, stride);
+      return;
+    }
+  }
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, wave = tid / kWave, r = tid / kLanes, c = tid % kLanes;
   const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * runs;
@@ -555,32 +635,6 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams 
   for (int i = 0; i < 2; ++i) w[i] = sum == 0.f ? 0u : pack2<T>(acc[2 * i] * k, acc[2 * i + 1] * k);
   *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * p.d + blockIdx.y * DIMS + c * 4) = w;
   if (p.lse && c == 0 && blockIdx.y == 0) p.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
-  if (sums && c == 0 && blockIdx.y == 0) *reinterpret_cast<f32x2*>(sums + row * 2) = f32x2{M, sum};
-}
-
-// mass[b, kh, t] += sum over the heads of kh of p_t / sum_j p_j: 1024 tokens a
-// block, four a thread, the heads one after another.
-constexpr int kMassTokens = 1024;
-__global__ __launch_bounds__(256) void attend_mass_kernel(AttendParams p, const float* scores, int64_t stride, const float* sums) {
-  const int b = blockIdx.z, kh = blockIdx.y, group = p.hq / p.hk;
-  const int hi = max(0, int(min(int64_t(p.lengths[b]), p.max_length)));
-  const int lo = p.window > 0 ? max(0, hi - p.window) : 0;
-  const int64_t at = int64_t(blockIdx.x) * kMassTokens + threadIdx.x * 4, t = lo / kTile * kTile + at;
-  if (t >= hi) return;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  const int64_t row0 = int64_t(b) * p.hq + int64_t(kh) * group;
-  for (int h = 0; h < group; ++h) {
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(sums + (row0 + h) * 2);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(scores + (row0 + h) * stride + at);
-    if (ml[1] == 0.f) continue;               // no score above -inf
-    const float k = 1.f / ml[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = fmaf(__builtin_amdgcn_exp2f(x[i] - ml[0]), k, acc[i]);
-  }
-  float* mass = p.mass + (int64_t(b) * p.hk + kh) * p.mass_span + t;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (t + i >= lo && t + i < hi) mass[i] += acc[i];
 }
 
 // How the tokens of the longest sequence are cut into runs, by what was
@@ -613,45 +667,45 @@ int64_t span_of(int64_t max_length, int64_t window) {
 
 // Where a call's workspace holds what, in floats.
 struct Layout {
-  int64_t part_o, scores, sums, end, stride;
+  bool whole;                     // one launch writes all
+  int64_t part_o, scores, end, stride;
 };
-Layout layout(const Plan& c, int64_t rows, int64_t d, bool mass) {
+Layout layout(const Plan& c, int64_t batch, int64_t hq, int64_t hk, int64_t d, bool mass) {
+  const int64_t rows = batch * hq;
   Layout l;
-  l.part_o = c.runs == 1 ? 0 : (rows * c.runs * 2 + 63) / 64 * 64;
-  l.scores = c.runs == 1 ? 0 : l.part_o + (rows * c.runs * d + 63) / 64 * 64;
+  l.whole = c.runs == 1 && (!mass || hq / hk <= 16);
+  l.part_o = l.whole ? 0 : (rows * c.runs * 2 + 63) / 64 * 64;
+  l.scores = l.whole ? 0 : l.part_o + (mass ? (rows * c.runs * d + 63) / 64 * 64 : rows * c.runs * d);
   l.stride = int64_t(c.runs) * c.tiles_per_run * kTile;
-  l.sums = l.scores + (mass ? rows * l.stride : 0);
-  l.end = l.sums + (mass ? rows * 2 : 0);
+  l.end = l.scores + (mass ? rows * l.stride : 0);
   return l;
+}
+
+template <class T, int DIMS, int THREADS, bool MASS>
+void launch_join(const AttendParams& p, const Plan& c, const Layout& l, float* ws, hipStream_t stream) {
+  const int64_t rows = int64_t(p.batch) * p.hq, y = p.d / DIMS;
+  const int64_t blocks = MASS ? int64_t(p.batch) * p.hk * ((l.stride + THREADS - 1) / THREADS) : 0;
+  attend_join_kernel<T, DIMS, THREADS, MASS><<<dim3(unsigned(rows + (blocks + y - 1) / y), unsigned(y)), dim3(THREADS), c.runs * sizeof(float), stream>>>(
+      p, c.runs, ws + l.part_o, ws, ws + l.scores, l.stride);
 }
 
 template <class T, Held C, int D, int W, bool UNI, bool MASS>
 hipError_t launch_form(const AttendParams& p, const Plan& c, hipStream_t stream) {
-  const int64_t rows = int64_t(p.batch) * p.hq;
-  const Layout l = layout(c, rows, D, MASS);
-  float* part_ml = static_cast<float*>(p.workspace);
-  float *part_o = part_ml + l.part_o, *scores = MASS ? part_ml + l.scores : nullptr, *sums = MASS ? part_ml + l.sums : nullptr;
+  const Layout l = layout(c, p.batch, p.hq, p.hk, D, MASS);
+  float* ws = static_cast<float*>(p.workspace);
   // Blocks go to the eight XCDs in turn: with an odd count of them a sequence, the
   // runs that short sequences lack are missing from all alike (16 sequences of
   // 1 to 65536 tokens in 32 runs 246 us, with a block more 221).  One sequence
   // lacks none, and its blocks are as many as fill the chip evenly (131072
   // tokens e4m3 31 us, with a block more 36).
   const dim3 grid(unsigned(p.batch > 1 ? c.runs | 1 : c.runs), unsigned(p.hk * ((p.hq / p.hk + 15) / 16)), unsigned(p.batch));
-  attend_kernel<T, C, D, W, UNI, MASS><<<grid, dim3(64 * W), 0, stream>>>(p, c.tiles_per_run, c.runs, part_o, part_ml, scores, sums);
+  attend_kernel<T, C, D, W, UNI, MASS><<<grid, dim3(64 * W), 0, stream>>>(p, c.tiles_per_run, c.runs, ws + l.part_o, ws, ws + l.scores);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (c.runs > 1) {
-    // Few rows: more blocks, each of a part of the dims (28 rows, 256 runs of 128
-    // dims 5.1 -> 2.9 us); many rows need no more blocks (896 rows, 4 runs: 5 us more).
-    if (rows < 256)
-      attend_join_kernel<T, 32, 512><<<dim3(unsigned(rows), D / 32), dim3(512), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml, sums);
-    else
-      attend_join_kernel<T, D, 256><<<dim3(unsigned(rows), 1), dim3(256), c.runs * sizeof(float), stream>>>(p, c.runs, part_o, part_ml, sums);
-    e = hipGetLastError();
-  }
-  if (!MASS || e != hipSuccess) return e;
-  attend_mass_kernel<<<dim3(unsigned((l.stride + kMassTokens - 1) / kMassTokens), unsigned(p.hk), unsigned(p.batch)), dim3(256), 0, stream>>>(
-      p, scores, l.stride, sums);
+  if (e != hipSuccess || l.whole) return e;
+  // Few rows: more blocks, each of a part of the dims (28 rows, 256 runs of 128
+  // dims 5.1 -> 2.9 us); many rows need no more blocks (896 rows, 4 runs: 5 us more).
+  if (int64_t(p.batch) * p.hq < 256) launch_join<T, 32, 512, MASS>(p, c, l, ws, stream);
+  else launch_join<T, D, 256, MASS>(p, c, l, ws, stream);
   return hipGetLastError();
 }
 
