@@ -227,12 +227,19 @@ struct RawKey<T, Held::kE2m1, D> {
 // part of 0: bfloat16's parts are cut below what they are parts of, so that
 // there is always a rest (p from 2^-90 on), and a float16 p's rest meets the
 // values through finite2.
-template <class T> constexpr int kParts = 3;
-template <> constexpr int kParts<F16> = 2;
-template <class T>
+// Values of 4 bits are finite, and what out's rounding to 2^-9 leaves of p is well
+// within two parts' 2^-18.
+template <class T, Held C> constexpr int kParts = std::is_same_v<T, Bf16> && C != Held::kE2m1 ? 3 : 2;
+template <class T, int PARTS>
 __device__ __forceinline__ void split(float a, float b, uint32_t* part);
 template <>
-__device__ __forceinline__ void split<Bf16>(float a, float b, uint32_t* part) {
+__device__ __forceinline__ void split<Bf16, 2>(float a, float b, uint32_t* part) {
+  part[0] = pack2<Bf16>(a, b);
+  const float2 r = unpack2<Bf16>(part[0]);
+  part[1] = pack2<Bf16>(a - r.x, b - r.y);
+}
+template <>
+__device__ __forceinline__ void split<Bf16, 3>(float a, float b, uint32_t* part) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     // The float below, or 0.
@@ -244,7 +251,7 @@ __device__ __forceinline__ void split<Bf16>(float a, float b, uint32_t* part) {
   part[2] = pack2<Bf16>(a, b);
 }
 template <>
-__device__ __forceinline__ void split<F16>(float a, float b, uint32_t* part) {
+__device__ __forceinline__ void split<F16, 2>(float a, float b, uint32_t* part) {
   part[0] = pack2<F16>(a, b);
   const float2 r = unpack2<F16>(part[0]);
   part[1] = pack2<F16>(a - r.x, b - r.y);
@@ -318,21 +325,22 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     return (page * unsigned(p.hk) + unsigned(kh)) * unsigned(p.page) + unsigned(t - page_index(t) * p.page);
   };
   // Row of the tile's token i, where lanes of a group want different ones.
-  auto row = [&](unsigned mine, int i, int bytes) {
-    return UNI ? uint64_t(mine) * bytes + unsigned(i) * bytes : uint64_t(unsigned(__shfl(int(mine), i))) * bytes;
-  };
+  auto row = [&](unsigned mine, int i) { return UNI ? uint64_t(mine) + unsigned(i) : uint64_t(unsigned(__shfl(int(mine), i))); };
   RawKey<T, C, D> key[2];
   RawValue<T, C, D> val[8];
   auto load_keys = [&](unsigned mine) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) key[i].load(kc + row(mine, i * 16 + c, kRow), p.k_exps + (kExps ? row(mine, i * 16 + c, kExps) : 0), g);
+    for (int i = 0; i < 2; ++i) {
+      const uint64_t r = row(mine, i * 16 + c);
+      key[i].load(kc + r * kRow, p.k_exps + r * kExps, g);
+    }
     keep_loads_here();
   };
   auto load_values = [&](unsigned mine) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int t = i / 4 * 16 + g * 4 + i % 4;
-      val[i].load(vc + row(mine, t, kRow), p.v_exps + (kExps ? row(mine, t, kExps) : 0), c);
+      const uint64_t r = row(mine, i / 4 * 16 + g * 4 + i % 4);
+      val[i].load(vc + r * kRow, p.v_exps + r * kExps, c);
     }
     keep_loads_here();
   };
@@ -392,15 +400,16 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     }
     // While no score is above -inf, each p is 0.
     const float base = m == -INFINITY ? 0.f : m;
-    u32x4 part[kParts<T>];
+    constexpr int kOf = kParts<T, C>;
+    u32x4 part[kOf];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float a = __builtin_amdgcn_exp2f(x[i] - base), e = __builtin_amdgcn_exp2f(x[i + 1] - base);
       l += a + e;
-      uint32_t w[kParts<T>];
-      split<T>(a, e, w);
+      uint32_t w[kOf];
+      split<T, kOf>(a, e, w);
 #pragma unroll
-      for (int n = 0; n < kParts<T>; ++n) part[n][i / 2] = w[n];
+      for (int n = 0; n < kOf; ++n) part[n][i / 2] = w[n];
     }
 #pragma unroll
     for (int i = 0; i < L::pairs; ++i) {
@@ -412,7 +421,7 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
         odd[j] = __builtin_amdgcn_perm(e, a, 0x07060302u);
       }
 #pragma unroll
-      for (int n = 0; n < kParts<T>; ++n) {
+      for (int n = 0; n < kOf; ++n) {
         if (std::is_same_v<T, F16> && C == Held::kSame && n == 1) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
