@@ -522,56 +522,67 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   }
 }
 
-// mass[b, kh, t] += sum over the heads of kh of p_t / sum_j p_j, a token a thread:
-// block `id` has THREADS consecutive ones of a (sequence, key-value head).  Its
-// waves find sixteen heads' maxima and sums from those of their runs, then all add up the heads.
+// mass[b, kh, t] += sum over the heads of kh of p_t / sum_j p_j, two tokens a thread:
+// block `id` has 2 THREADS consecutive ones of a (sequence, key-value head).  Its waves
+// find sixteen heads' maxima and sums from those of their runs, while the scores are on
+// their way, then all add up the heads.
 template <int THREADS>
 __device__ __forceinline__ void add_mass(const AttendParams& p, int64_t id, int runs, const float* part_ml, const float* scores,
                                          int64_t stride) {
   __shared__ float s_top[16], s_rec[16];
-  const int64_t chunks = (stride + THREADS - 1) / THREADS, bk = id / chunks;
+  const int64_t chunks = (stride + 2 * THREADS - 1) / (2 * THREADS), bk = id / chunks;
   if (bk >= int64_t(p.batch) * p.hk) return;
-  const int64_t b = bk / p.hk, at = (id - bk * chunks) * THREADS + threadIdx.x;
+  const int64_t b = bk / p.hk, at = (id - bk * chunks) * (2 * THREADS) + threadIdx.x;
   const int kh = int(bk - b * p.hk), group = p.hq / p.hk, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hi = max(0, int(min(int64_t(p.lengths[b]), p.max_length)));
   const int lo = p.window > 0 ? max(0, hi - p.window) : 0;
   const int64_t t = lo / kTile * kTile + at;
   if (t - int(threadIdx.x) >= hi) return;
-  const bool here = t >= lo && t < hi;
   const int64_t row0 = b * p.hq + int64_t(kh) * group;
   float* mass = p.mass + bk * p.mass_span + t;
-  const float before = here ? *mass : 0.f;
-  float more = 0.f;
+  bool here[2];
+  float before[2], more[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    here[i] = t + i * THREADS >= lo && t + i * THREADS < hi;
+    before[i] = here[i] ? mass[i * THREADS] : 0.f;
+  }
   for (int h0 = 0; h0 < group; h0 += 16) {
     const int heads = min(16, group - h0);
-    float x[16];
+    float x[2][16];
 #pragma unroll
-    for (int h = 0; h < 16; ++h) x[h] = h < heads && here ? scores[(row0 + h0 + h) * stride + at] : 0.f;
+    for (int h = 0; h < 16; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) x[i][h] = h < heads && here[i] ? scores[(row0 + h0 + h) * stride + at + i * THREADS] : 0.f;
     for (int h = wave; h < heads; h += THREADS / kWave) {
       const float2* ml = reinterpret_cast<const float2*>(part_ml) + (row0 + h0 + h) * runs;
       float M = -INFINITY, sum = 0.f;
+#pragma unroll 4
       for (int s = lane; s < runs; s += kWave) {
         const float2 v = ml[s];
-        if (v.y != 0.f) M = fmaxf(M, v.x);
+        if (v.y == 0.f) continue;
+        const float top = fmaxf(M, v.x);
+        sum = fmaf(v.y, __builtin_amdgcn_exp2f(v.x - top), sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f(M - top));
+        M = top;
       }
-      M = wave_max(M);
-      for (int s = lane; s < runs; s += kWave) {
-        const float2 v = ml[s];
-        if (v.y != 0.f) sum = fmaf(v.y, __builtin_amdgcn_exp2f(v.x - M), sum);
-      }
-      sum = wave_sum(sum);
+      const float top = wave_max(M);
+      sum = wave_sum(sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f(M - top));
       if (lane == 0) {
-        s_top[h] = M;
+        s_top[h] = top;
         s_rec[h] = sum == 0.f ? 0.f : 1.f / sum;      // 0: no score above -inf
       }
     }
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 16; ++h)
-      if (h < heads && s_rec[h] != 0.f) more = fmaf(__builtin_amdgcn_exp2f(x[h] - s_top[h]), s_rec[h], more);
+      if (h < heads && s_rec[h] != 0.f)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) more[i] = fmaf(__builtin_amdgcn_exp2f(x[i][h] - s_top[h]), s_rec[h], more[i]);
     if (h0 + 16 < group) __syncthreads();
   }
-  if (here) *mass = before + more;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (here[i]) mass[i * THREADS] = before[i] + more[i];
 }
 
 // The runs of one (sequence, query head) joined, DIMS dims a block.  The runs'
@@ -693,7 +704,7 @@ Layout layout(const Plan& c, int64_t batch, int64_t hq, int64_t hk, int64_t d, b
 template <class T, int DIMS, int THREADS, bool MASS>
 void launch_join(const AttendParams& p, const Plan& c, const Layout& l, float* ws, hipStream_t stream) {
   const int64_t rows = int64_t(p.batch) * p.hq, y = p.d / DIMS;
-  const int64_t blocks = MASS ? int64_t(p.batch) * p.hk * ((l.stride + THREADS - 1) / THREADS) : 0;
+  const int64_t blocks = MASS ? int64_t(p.batch) * p.hk * ((l.stride + 2 * THREADS - 1) / (2 * THREADS)) : 0;
   attend_join_kernel<T, DIMS, THREADS, MASS><<<dim3(unsigned(rows + (blocks + y - 1) / y), unsigned(y)), dim3(THREADS), c.runs * sizeof(float), stream>>>(
       p, c.runs, ws + l.part_o, ws, ws + l.scores, l.stride);
 }
