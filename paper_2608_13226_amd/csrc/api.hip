@@ -773,13 +773,13 @@ static cp_status check_attend(int64_t batch, int64_t hq, int64_t hk, int64_t d, 
 size_t coverprune_paged_attention_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                             int64_t window) {
   if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
-  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, false);
+  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, false, false);
 }
 
 size_t coverprune_paged_attention_mass_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                                  int64_t window) {
   if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
-  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, true);
+  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, true, false);
 }
 
 // Pages, table and lengths of a call over a paged cache.
@@ -810,7 +810,7 @@ static cp_status attend(bool mass, cp::AttendParams& p, cp_dtype dtype, int64_t 
   if (mass && !p.mass) return fail(CP_ERR_INVALID_ARG, "mass must be non-NULL");
   if (!aligned16(p.q) || !aligned16(p.k_cache) || !aligned16(p.v_cache) || !aligned16(p.out) || (mass && !aligned16(p.mass)))
     return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, out and mass must be 16-byte aligned");
-  if ((st = check_workspace(p.workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, p.max_length, window, mass))) != CP_OK)
+  if ((st = check_workspace(p.workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, p.max_length, window, mass, held == CP_E2M1))) != CP_OK)
     return st;
   p.batch = int(batch);
   p.hq = int(hq);

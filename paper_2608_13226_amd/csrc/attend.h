@@ -274,8 +274,9 @@ __device__ __forceinline__ void keep_loads_here() { asm volatile("" ::: "memory"
 // memory and its address is the wave's; otherwise each lane finds one token's
 // row and the lanes exchange them.
 template <class T, Held C, int D, int W, bool UNI, bool MASS>
-__global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
-                                                           float* part_ml, float* scores) {
+__global__ __launch_bounds__(64 * W, W == 16 ? 1 : 2) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
+                                                           float* part_ml, float* scores, bool whole) {
+  extern __shared__ float s_x[];                // MASS, whole: the scores [heads][tokens]
   constexpr int kSteps = D / 32;
   using L = Dims<D>;
   __shared__ float s_o[W][16][D + 4];
@@ -380,7 +381,8 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     }
     if constexpr (MASS) {
       if (c < heads) {
-        float* to = scores + (int64_t(b) * p.hq + h0 + c) * (int64_t(runs) * tiles_per_run * kTile) + int64_t(tile - lo / kTile) * kTile + g * 4;
+        const int64_t stride = int64_t(runs) * tiles_per_run * kTile;
+        float* to = (whole ? s_x + c * stride : scores + (int64_t(b) * p.hq + h0 + c) * stride) + int64_t(tile - lo / kTile) * kTile + g * 4;
 #pragma unroll
         for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(to + i * 16) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
       }
@@ -473,8 +475,10 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
   }
   __syncthreads();
   const float vs = p.v_scale ? p.v_scale[kh] : 1.f;
-  // Whether this block has all that there is of its heads (and, for the masses, of its key-value head).
-  const bool whole = runs == 1 && (!MASS || group <= 16);
+  // The token whose mass this thread adds to, in a block that has all of its key-value head.
+  int t = lo + int(threadIdx.x);
+  float* mass = MASS ? p.mass + (int64_t(b) * p.hk + kh) * p.mass_span : nullptr;
+  float before = MASS && whole && t < hi ? mass[t] : 0.f;
   for (int i = threadIdx.x; i < heads * (D / 4); i += 64 * W) {
     const int h = i / (D / 4), d = i % (D / 4) * 4;
     float M = s_m[0][h];
@@ -507,18 +511,15 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(AttendParams p, int t
     }
   }
   if (!MASS || !whole) return;
-  // The scores that this block left, all of its key-value head's.
-  __syncthreads();
-  float* mass = p.mass + (int64_t(b) * p.hk + kh) * p.mass_span;
-  for (int t = lo + int(threadIdx.x); t < hi; t += 64 * W) {
-    const float* x = scores + (int64_t(b) * p.hq + h0) * (int64_t(tiles_per_run) * kTile) + (t - lo / kTile * kTile);
+  lds_sync();
+  for (; t < hi; t += 64 * W) {
+    const float* x = s_x + (t - lo / kTile * kTile);
     float more = 0.f;
 #pragma unroll 4
-    for (int h = 0; h < heads; ++h) {
-      const float score = x[int64_t(h) * tiles_per_run * kTile];
-      if (s_sum[h] != 0.f) more = fmaf(__builtin_amdgcn_exp2f(score - s_top[h]), 1.f / s_sum[h], more);
-    }
-    mass[t] += more;
+    for (int h = 0; h < heads; ++h)
+      if (s_sum[h] != 0.f) more = fmaf(__builtin_amdgcn_exp2f(x[h * tiles_per_run * kTile] - s_top[h]), 1.f / s_sum[h], more);
+    mass[t] = before + more;
+    before = t + 64 * W < hi ? mass[t + 64 * W] : 0.f;
   }
 }
 
@@ -670,9 +671,10 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendParams 
 struct Plan {
   int tiles_per_run, runs, waves;
 };
-Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span) {
+Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span, bool four) {
   const int64_t tiles = (span + kTile - 1) / kTile;
   const int64_t blocks = batch * hk * ((hq / hk + 15) / 16);
+  if (four && tiles > 16 && tiles <= 24) return {int(tiles), 1, 16};
   if (tiles <= (blocks >= 64 ? 32 : 16)) return {int(tiles), 1, tiles > 4 ? 8 : 4};
   const int64_t want = (std::min<int64_t>(2048, 512 * batch) + blocks - 1) / blocks;
   int64_t per = std::max<int64_t>(blocks <= 16 ? 4 : 8, (tiles + want - 1) / want);
@@ -687,17 +689,18 @@ int64_t span_of(int64_t max_length, int64_t window) {
 
 // Where a call's workspace holds what, in floats.
 struct Layout {
-  bool whole;                     // one launch writes all
+  bool whole;                     // one launch writes all; with masses the scores are in its blocks' LDS
   int64_t part_o, scores, end, stride;
 };
 Layout layout(const Plan& c, int64_t batch, int64_t hq, int64_t hk, int64_t d, bool mass) {
   const int64_t rows = batch * hq;
   Layout l;
-  l.whole = c.runs == 1 && (!mass || hq / hk <= 16);
+  l.stride = int64_t(c.runs) * c.tiles_per_run * kTile;
+  const int64_t lds = c.waves * 16 * (d + 4 + 2) + 64 + hq / hk * l.stride;
+  l.whole = c.runs == 1 && (!mass || (hq / hk <= 16 && lds * int64_t(sizeof(float)) <= 160 * 1024));
   l.part_o = l.whole ? 0 : (rows * c.runs * 2 + 63) / 64 * 64;
   l.scores = l.whole ? 0 : l.part_o + (mass ? (rows * c.runs * d + 63) / 64 * 64 : rows * c.runs * d);
-  l.stride = int64_t(c.runs) * c.tiles_per_run * kTile;
-  l.end = l.scores + (mass ? rows * l.stride : 0);
+  l.end = l.scores + (mass && !l.whole ? rows * l.stride : 0);
   return l;
 }
 
@@ -719,7 +722,8 @@ hipError_t launch_form(const AttendParams& p, const Plan& c, hipStream_t stream)
   // lacks none, and its blocks are as many as fill the chip evenly (131072
   // tokens e4m3 31 us, with a block more 36).
   const dim3 grid(unsigned(p.batch > 1 ? c.runs | 1 : c.runs), unsigned(p.hk * ((p.hq / p.hk + 15) / 16)), unsigned(p.batch));
-  attend_kernel<T, C, D, W, UNI, MASS><<<grid, dim3(64 * W), 0, stream>>>(p, c.tiles_per_run, c.runs, ws + l.part_o, ws, ws + l.scores);
+  const size_t lds = MASS && l.whole ? size_t(p.hq / p.hk * l.stride) * sizeof(float) : 0;
+  attend_kernel<T, C, D, W, UNI, MASS><<<grid, dim3(64 * W), lds, stream>>>(p, c.tiles_per_run, c.runs, ws + l.part_o, ws, ws + l.scores, l.whole);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || l.whole) return e;
   // Few rows: more blocks, each of a part of the dims (28 rows, 256 runs of 128
@@ -731,7 +735,11 @@ hipError_t launch_form(const AttendParams& p, const Plan& c, hipStream_t stream)
 
 template <class T, Held C, int D, bool MASS>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  const Plan c = plan(p.batch, p.hq, p.hk, span_of(p.max_length, p.window));
+  constexpr bool kFour = C == Held::kE2m1 && D <= 128;
+  const Plan c = plan(p.batch, p.hq, p.hk, span_of(p.max_length, p.window), kFour);
+  if constexpr (kFour)
+    if (c.waves == 16)
+      return p.page % kTile == 0 ? launch_form<T, C, D, 16, true, MASS>(p, c, stream) : launch_form<T, C, D, 16, false, MASS>(p, c, stream);
   if (p.page % kTile == 0)
     return c.waves == 8 ? launch_form<T, C, D, 8, true, MASS>(p, c, stream) : launch_form<T, C, D, 4, true, MASS>(p, c, stream);
   return c.waves == 8 ? launch_form<T, C, D, 8, false, MASS>(p, c, stream) : launch_form<T, C, D, 4, false, MASS>(p, c, stream);

@@ -4,8 +4,8 @@
 
 namespace cp {
 
-size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass) {
-  return size_t(layout(plan(batch, hq, hk, span_of(max_length, window)), batch, hq, hk, d, mass).end) * sizeof(float);
+size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass, bool four) {
+  return size_t(layout(plan(batch, hq, hk, span_of(max_length, window), four && d <= 128), batch, hq, hk, d, mass).end) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream) {

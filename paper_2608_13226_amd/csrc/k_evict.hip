@@ -42,13 +42,6 @@ __device__ __forceinline__ uint32_t rank_of(float m) {
 
 __device__ __forceinline__ int tokens_of(const KvEvictParams& p, int b) { return max(0, int(min(int64_t(p.lengths[b]), p.max_length))); }
 
-// A workgroup barrier that orders LDS alone: what goes to and from memory stays under way.
-__device__ __forceinline__ void lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // How many lanes below this one have their bit in `ballot`.
 __device__ __forceinline__ int lanes_below(unsigned long long ballot) {
   return int(__builtin_amdgcn_mbcnt_hi(unsigned(ballot >> 32), __builtin_amdgcn_mbcnt_lo(unsigned(ballot), 0u)));

@@ -329,7 +329,7 @@ struct AttendParams {
   void* workspace;
 };
 // 0 where one launch writes the result.
-size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass);
+size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass, bool four);
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
 hipError_t launch_attend4(const AttendParams& p, hipStream_t stream);
 hipError_t launch_attend_mass(const AttendParams& p, hipStream_t stream);

@@ -166,6 +166,13 @@ __device__ __forceinline__ void store4<E4m3>(void* p, int64_t i, const float* x)
   *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = pack4_e4m3(x[0], x[1], x[2], x[3]);
 }
 
+// A workgroup barrier that orders LDS alone: what goes to and from memory stays under way.
+__device__ __forceinline__ void lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
