@@ -948,6 +948,8 @@ cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, 
   p.d = int(d);
   p.rot = int(rot);
   p.page = int(page_size);
+  p.by_page = cp::Divide(page_size);
+  p.by_runs = cp::Divide(d / 8);
   p.magnitude = magnitude;
   p.interleaved = interleaved != 0;
   serve_type(dtype, &p.type);
@@ -990,6 +992,7 @@ cp_status coverprune_kv_gather(const void* k_cache, const void* v_cache, cp_dtyp
   p.hk = int(hk);
   p.d = int(d);
   p.page = int(page_size);
+  p.by_page = cp::Divide(page_size);
   serve_type(dtype, &p.type);
   serve_type(cache_dtype, &p.held);
   hipError_t e = cp::launch_kv_gather(p, static_cast<hipStream_t>(stream));
@@ -1060,6 +1063,7 @@ cp_status coverprune_kv_evict(void* k_cache, void* v_cache, cp_dtype cache_dtype
   p.hk = int(hk);
   p.page = int(page_size);
   p.width = int(width);
+  p.by_page = cp::Divide(page_size);
   p.row_bytes = int(four ? d / 2 : cache_dtype == CP_E4M3 ? d : 2 * d);
   p.exp_bytes = int(four ? d / 32 : 0);
   p.workspace = workspace;

@@ -21,14 +21,12 @@
 namespace cp {
 namespace {
 
-// float64 to float32, rounded to odd; numbers past float32's range become its largest.
+// float64 to float32, rounded to odd: of the 29 bits that go, whether any was set stays in the
+// last one of the others, and the conversion is exact.  (Past float32's range: infinite.)
 __device__ __forceinline__ float round_odd(double x) {
-  const float r = float(x);
-  const uint32_t bits = __float_as_uint(r);
-  if (double(r) == x || x != x) return r;
-  if (__builtin_isinf(x)) return r;
-  // |r| above |x|: one step back (from infinity to the largest number).
-  return __uint_as_float((bits - (fabs(double(r)) > fabs(x) ? 1u : 0u)) | 1u);
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t low = uint32_t(b), kept = (low & 0xe0000000u) | (low & 0x1fffffffu ? 0x20000000u : 0u);
+  return float(__builtin_bit_cast(double, (b & 0xffffffff00000000u) | kept));
 }
 
 // Eight elements from element i on.
@@ -55,8 +53,8 @@ __device__ __forceinline__ uint32_t cut_block(const float* x, uint32_t* exponent
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-  top = max(top, uint32_t(__shfl_xor(int(top), 1)));
-  top = max(top, uint32_t(__shfl_xor(int(top), 2)));
+  top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xb1, 0xf, 0xf, true)));     // lane ^ 1
+  top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x4e, 0xf, 0xf, true)));     // lane ^ 2
   if (top >= 0x7f800000u) {
     *exponent = 255u;
     return 0u;
@@ -142,10 +140,10 @@ __global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int 
   __syncthreads();
   if (!here) return;
   const int runs = p.d / 8, hq = p.q ? p.hq : 0;
-  const int64_t pg = keep ? slot / p.page : 0, off = keep ? slot - pg * p.page : 0;
+  const int64_t pg = keep ? page_of(slot, p.page, p.by_page) : 0, off = keep ? slot - pg * p.page : 0;
   const int total = (hq + (keep ? 2 * p.hk : 0)) * runs;
   for (int w = int(blockIdx.y) * threads + tid; w < total; w += int(gridDim.y) * threads) {
-    const int head = w / runs, e = (w - head * runs) * 8;
+    const int head = int(p.by_runs(unsigned(w))), e = (w - head * runs) * 8;
     if (head < hq) {
       const int64_t from = t * p.q_stride + int64_t(head) * p.d;
       float x[8], y[8];
@@ -163,8 +161,19 @@ __global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int 
     if (is_k) {
       double y[8];
       turn_run<T, INTER, WIDE, double>(src, from, e, p.rot, s_cos, s_sin, x, y);
+      if (e < p.rot) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = round_odd(y[j]);
+        for (int j = 0; j < 8; ++j) x[j] = round_odd(y[j]);
+        // What is finite but past float32's range counts as its largest number.
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
+        if (most > 3e38f) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (fabs(y[j]) < __builtin_inf()) x[j] = float(fmin(fmax(y[j], -3.4028234663852886e38), 3.4028234663852886e38));
+        }
+      }
     }
     uint32_t exponent;
     const uint32_t codes = cut_block<T>(x, &exponent);

@@ -109,7 +109,7 @@ struct Place {
   int b, kh;
   // Row of token t.
   __device__ __forceinline__ uint32_t row(int t) const {
-    const int page = t / p.page;
+    const int page = int(p.by_page(unsigned(t)));
     const unsigned entry = min(unsigned(p.table[int64_t(b) * p.width + page]), unsigned(p.pages - 1));
     return (entry * unsigned(p.hk) + unsigned(kh)) * unsigned(p.page) + unsigned(t - page * p.page);
   }

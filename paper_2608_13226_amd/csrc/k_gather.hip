@@ -71,9 +71,9 @@ struct Run {
   }
 };
 
-// `tokens` tokens a block: a_token = 2 hk runs of them each, so that a run's token comes from a 32-bit division.
+// `tokens` tokens a block, of a_token runs each.
 template <class T, int BITS, int VEC>
-__global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, int tokens, int64_t first_block) {
+__global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, Divide by_token, Divide by_runs, int tokens, int64_t first_block) {
   const unsigned runs = unsigned(p.d / VEC), half = unsigned(p.hk) * runs, a_token = 2 * half;
   const int64_t t0 = (first_block + blockIdx.x) * tokens;
   const unsigned total = unsigned(min(int64_t(tokens), p.tokens - t0)) * a_token;
@@ -81,21 +81,20 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(KvGatherParams p, int to
     Run<T, BITS, VEC> x[kAhead];
     int64_t slot[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) slot[i] = p.slots[t0 + min(w0 + i * 256, total - 1) / a_token];
+    for (int i = 0; i < kAhead; ++i) slot[i] = p.slots[t0 + by_token(min(w0 + i * 256, total - 1))];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const unsigned w = min(w0 + i * 256, total - 1), r = w % a_token, in = r < half ? r : r - half;
-      const unsigned kh = in / runs, e = (in - kh * runs) * VEC;
+      const unsigned w = min(w0 + i * 256, total - 1), r = w - by_token(w) * a_token, in = r < half ? r : r - half;
+      const unsigned kh = by_runs(in), e = (in - kh * runs) * VEC;
       const int64_t at = slot[i] >= 0 && slot[i] < p.pages * p.page ? slot[i] : 0;
-      // (Slots past 2^32 want a division of 64 bits.)
-      const int64_t pg = uint64_t(at) >> 32 ? at / p.page : int64_t(uint32_t(at) / uint32_t(p.page));
+      const int64_t pg = page_of(at, p.page, p.by_page);
       x[i].load(p, r >= half, (pg * p.hk + kh) * p.page + (at - pg * p.page), int(kh), int(e));
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const unsigned w = w0 + i * 256;
       if (w >= total) break;
-      const unsigned token = w / a_token, r = w - token * a_token, in = r < half ? r : r - half;
+      const unsigned token = by_token(w), r = w - token * a_token, in = r < half ? r : r - half;
       if (slot[i] < 0 || slot[i] >= p.pages * p.page) x[i] = {};
       x[i].store(r < half ? p.k_out : p.v_out, (t0 + token) * half * VEC + in * VEC);
     }
@@ -108,7 +107,7 @@ hipError_t launch(const KvGatherParams& p, hipStream_t stream) {
   const int64_t a_token = 2 * int64_t(p.hk) * (p.d / VEC);
   const int tokens = int(std::max<int64_t>(1, 256 * kAhead / a_token));
   return launch_blocks((p.tokens + tokens - 1) / tokens, 256, [&](int64_t first, unsigned blocks) {
-    kv_gather_kernel<T, BITS, VEC><<<dim3(blocks), dim3(256), 0, stream>>>(p, tokens, first);
+    kv_gather_kernel<T, BITS, VEC><<<dim3(blocks), dim3(256), 0, stream>>>(p, Divide(a_token), Divide(p.d / VEC), tokens, first);
   });
 }
 

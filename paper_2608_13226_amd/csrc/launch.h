@@ -266,6 +266,18 @@ struct KvAppendParams {
 };
 hipError_t launch_kv_append(const KvAppendParams& p, hipStream_t stream);
 
+// n / d for 0 <= n < 2^31 without a division: (2 n * magic >> 32) >> shift, with shift =
+// ceil(log2 d) and magic = ceil(2^(31 + shift) / d).
+struct Divide {
+  unsigned magic = 0, shift = 0;
+  Divide() = default;
+  explicit Divide(int64_t d) {
+    while ((int64_t(1) << shift) < d) ++shift;
+    magic = unsigned(((int64_t(1) << (31 + shift)) + d - 1) / d);
+  }
+  __host__ __device__ unsigned operator()(unsigned n) const { return unsigned(uint64_t(2u * n) * magic >> 32) >> shift; }
+};
+
 // The caches of 4 bits: codes two a byte, the even dim low, and exponents of blocks of 32 dims.
 struct KvAppend4Params {
   const void* q;                  // [tokens, hq, d] at token stride q_stride, or nullptr
@@ -282,6 +294,7 @@ struct KvAppend4Params {
   uint8_t* v_scale;
   int64_t tokens, pages;
   int hq, hk, d, rot, page;       // d % 32 == 0
+  Divide by_page, by_runs;        // by d / 8
   float magnitude;
   bool interleaved;
   ServeType type;
@@ -298,6 +311,7 @@ struct KvGatherParams {
   void* v_out;
   int64_t tokens, pages;
   int hk, d, page;
+  Divide by_page;
   ServeType type;                 // of the outputs
   ServeType held;                 // `type`, kE4m3 or kE2m1 (d % 32 == 0)
 };
@@ -349,6 +363,7 @@ struct KvEvictParams {
   int64_t span, pages, max_length;  // 1 <= max_length <= min(span, width * page) < 2^31
   int64_t keep, recent, sink;     // 1 <= keep < 2^31, 0 <= sink + recent <= keep
   int batch, hk, page, width;
+  Divide by_page;
   int row_bytes, exp_bytes;       // row_bytes a multiple of 8; exp_bytes 0 without exponents
   int row_shift;                  // these two are launch_kv_evict's
   bool exp_words;

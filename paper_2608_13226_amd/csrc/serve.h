@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "launch.h"
 
 namespace cp {
 
@@ -217,6 +218,11 @@ __device__ __forceinline__ uint32_t widen2<F16, true>(uint32_t w) {
 // element in the low half, times a power of two for each 32 elements, which is held as
 // its exponent plus 127; 255 makes a block NaN.
 constexpr int kBlock4 = 32;
+
+// The page of a slot, which is 0 or more.
+__device__ __forceinline__ int64_t page_of(int64_t slot, int page, const Divide& by_page) {
+  return uint64_t(slot) >> 31 ? slot / page : int64_t(by_page(unsigned(slot)));
+}
 
 // The power of two that an exponent byte stands for, as the conversions take it (they read its exponent alone).
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
