@@ -29,14 +29,22 @@ __device__ __forceinline__ float round_odd(double x) {
   return float(__builtin_bit_cast(double, (b & 0xffffffff00000000u) | kept));
 }
 
-// Eight elements from element i on.
-template <class T, bool WIDE>
-__device__ __forceinline__ void load_run(const void* p, int64_t i, float* x) {
-  if constexpr (WIDE) {
-    load8<T>(p, i, x);
-  } else {
+// Eight elements from element i on, as they are stored.
+template <bool WHOLE>
+__device__ __forceinline__ u32x4 load_run(const uint16_t* p) {
+  if constexpr (WHOLE) return *reinterpret_cast<const u32x4*>(p);
+  u32x4 w;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = load1<T>(p, i + j);
+  for (int j = 0; j < 4; ++j) w[j] = uint32_t(p[2 * j]) | uint32_t(p[2 * j + 1]) << 16;
+  return w;
+}
+template <class T>
+__device__ __forceinline__ void widen8(u32x4 w, float* x) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = unpack2<T>(w[j]);
+    x[2 * j] = f.x;
+    x[2 * j + 1] = f.y;
   }
 }
 
@@ -71,58 +79,75 @@ __device__ __forceinline__ uint32_t cut_block(const float* x, uint32_t* exponent
   return w;
 }
 
-// The run's elements e + 0..7 of a head whose first is element `head` of p, turned:
-// `own` holds them, cosines and sines of the pairs are cs[pair].  R: float or double.
-template <class T, bool INTER, bool WIDE, class R>
-__device__ __forceinline__ void turn_run(const void* p, int64_t head, int e, int rot, const R* cosines, const R* sines,
-                                         const float* own, R* y) {
+// Elements e + 0..7 of a head, which lie at `run`, turned where they are below rot; `own` holds
+// them, cosines and sines are the pairs'.  R: float or double.
+template <class T, bool INTER, bool WHOLE, class R>
+__device__ __forceinline__ void turn_run(const uint16_t* run, int e, int rot, const R* cosines, const R* sines, const float* own, R* y) {
   const int half = rot / 2;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = own[j];
-  if (e >= rot) return;
-  if constexpr (INTER) {
+  if constexpr (WHOLE && INTER) {
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-      if (e + j >= rot) break;
-      const R c = cosines[(e + j) / 2], s = sines[(e + j) / 2], a = own[j], b = own[j + 1];
+      const R c = cosines[e / 2 + j / 2], s = sines[e / 2 + j / 2], a = own[j], b = own[j + 1];
       y[j] = a * c - b * s;
       y[j + 1] = b * c + a * s;
     }
-  } else if (WIDE && half % 8 == 0) {
+  } else if constexpr (WHOLE) {
     const bool second = e >= half;
     const int i0 = second ? e - half : e;
     float other[8];
-    load_run<T, true>(p, head + (second ? i0 : e + half), other);
+    widen8<T>(load_run<true>(run + (second ? -half : half)), other);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const R c = cosines[i0 + j], s = sines[i0 + j], a = own[j], b = other[j];
-      y[j] = second ? a * c + b * s : a * c - b * s;
+      const R c = cosines[i0 + j], s = second ? -sines[i0 + j] : sines[i0 + j];
+      y[j] = R(own[j]) * c - R(other[j]) * s;
     }
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (e + j >= rot) break;
-      const bool second = e + j >= half;
-      const int i = second ? e + j - half : e + j;
-      const R c = cosines[i], s = sines[i], a = own[j], b = load1<T>(p, head + (second ? i : i + half));
-      y[j] = second ? a * c + b * s : a * c - b * s;
+      const int i = e + j;
+      y[j] = own[j];
+      if (i < rot) {
+        const bool second = INTER ? i % 2 != 0 : i >= half;
+        const int pair = INTER ? i / 2 : second ? i - half : i, to = INTER ? (second ? -1 : 1) : second ? -half : half;
+        const R c = cosines[pair], s = second ? -sines[pair] : sines[pair], other = load1<T>(run, j + to);
+        y[j] = R(own[j]) * c - other * s;
+      }
     }
   }
 }
 
-// A block of 256 has `threads` for each of its tokens; a thread has runs of eight
-// elements, queries' first, then keys', then values'.  WIDE: rows are 16-byte aligned.
-template <class T, bool INTER, bool WIDE>
-__global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int threads, int64_t first_block) {
+// A block of 256 has 2^shift threads, whole waves, for each of its tokens.  A thread has runs of
+// eight elements, queries', then keys', then values'; the first of each are on their way while the
+// block finds the token's angles.  WHOLE: rows are 16-byte aligned and no run holds the
+// end of a head's turned part or of its half.
+template <class T, bool INTER, bool WHOLE>
+__global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int shift, int64_t first_block) {
   extern __shared__ double s_turns[];         // a token's [rot / 2] cosines, sines, and both again as floats
-  const int tid = threadIdx.x % threads, mine = threadIdx.x / threads;
-  const int64_t token = (first_block + blockIdx.x) * (256 / threads) + mine, t = min(token, p.tokens - 1);
+  const int threads = 1 << shift, tid = int(threadIdx.x) & (threads - 1);
+  const int mine = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> shift);
+  const int64_t token = (first_block + blockIdx.x) * (256 >> shift) + mine, t = min(token, p.tokens - 1);
   const int half = p.rot / 2;
   double *s_cos = s_turns + int64_t(mine) * half * 3, *s_sin = s_cos + half;
   float *s_cosf = reinterpret_cast<float*>(s_sin + half), *s_sinf = s_cosf + half;
   const double position = double(p.positions[t]);
   const int64_t slot = p.slots[t];
-  const bool here = token < p.tokens, keep = here && slot >= 0 && slot < p.pages * p.page;
+
+  const int runs = p.d / 8, q_runs = p.q ? p.hq * runs : 0, k_runs = p.hk * runs;
+  const int step = int(gridDim.y) * threads, at = int(blockIdx.y) * threads + tid;
+  // The thread's first run of a tensor before which the threads have had `before`.
+  auto first_of = [&](int before) {
+    const int w = at - before % step;
+    return w < 0 ? w + step : w;
+  };
+  const int q0 = at, k0 = first_of(q_runs), v0 = first_of(q_runs + k_runs);
+  const uint16_t* q = static_cast<const uint16_t*>(p.q) + t * p.q_stride;
+  const uint16_t* k = static_cast<const uint16_t*>(p.k) + t * p.k_stride;
+  const uint16_t* v = static_cast<const uint16_t*>(p.v) + t * p.v_stride;
+  u32x4 raw_q = {0, 0, 0, 0}, raw_k = raw_q, raw_v = raw_q;
+  if (q0 < q_runs) raw_q = load_run<WHOLE>(q + q0 * 8);
+  if (k0 < k_runs) raw_k = load_run<WHOLE>(k + k0 * 8);
+  if (v0 < k_runs) raw_v = load_run<WHOLE>(v + v0 * 8);
+
   for (int i = tid; i < half; i += threads) {
     const double angle = position * double(p.inv_freq[i]);
     // angle / 2 pi less its whole turns; 1 / 2 pi = high + low.
@@ -137,61 +162,74 @@ __global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int 
     s_cosf[i] = float(c);
     s_sinf[i] = float(s);
   }
-  __syncthreads();
-  if (!here) return;
-  const int runs = p.d / 8, hq = p.q ? p.hq : 0;
-  const int64_t pg = keep ? page_of(slot, p.page, p.by_page) : 0, off = keep ? slot - pg * p.page : 0;
-  const int total = (hq + (keep ? 2 * p.hk : 0)) * runs;
-  for (int w = int(blockIdx.y) * threads + tid; w < total; w += int(gridDim.y) * threads) {
-    const int head = int(p.by_runs(unsigned(w))), e = (w - head * runs) * 8;
-    if (head < hq) {
-      const int64_t from = t * p.q_stride + int64_t(head) * p.d;
+  lds_sync();
+  if (token >= p.tokens) return;
+
+  uint16_t* q_out = static_cast<uint16_t*>(p.q_out) + t * (p.hq * int64_t(p.d));
+  for (int w = q0; w < q_runs; w += step) {
+    const int e = (w - int(p.by_runs(unsigned(w))) * runs) * 8;
+    if (w != q0) raw_q = load_run<WHOLE>(q + w * 8);
+    if (e < p.rot) {
       float x[8], y[8];
-      load_run<T, WIDE>(p.q, from + e, x);
-      turn_run<T, INTER, WIDE, float>(p.q, from, e, p.rot, s_cosf, s_sinf, x, y);
-      store8<T>(p.q_out, (t * p.hq + head) * p.d + e, y);
-      continue;
+      widen8<T>(raw_q, x);
+      turn_run<T, INTER, WHOLE, float>(q + w * 8, e, p.rot, s_cosf, s_sinf, x, y);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) raw_q[j] = pack2<T>(y[2 * j], y[2 * j + 1]);
     }
-    const bool is_k = head < hq + p.hk;
-    const int kh = head - hq - (is_k ? 0 : p.hk);
-    const void* src = is_k ? p.k : p.v;
-    const int64_t from = t * (is_k ? p.k_stride : p.v_stride) + int64_t(kh) * p.d;
-    float x[8];
-    load_run<T, WIDE>(src, from + e, x);
-    if (is_k) {
-      double y[8];
-      turn_run<T, INTER, WIDE, double>(src, from, e, p.rot, s_cos, s_sin, x, y);
-      if (e < p.rot) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = round_odd(y[j]);
-        // What is finite but past float32's range counts as its largest number.
-        float most = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));
-        if (most > 3e38f) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (fabs(y[j]) < __builtin_inf()) x[j] = float(fmin(fmax(y[j], -3.4028234663852886e38), 3.4028234663852886e38));
-        }
-      }
-    }
+    *reinterpret_cast<u32x4*>(q_out + w * 8) = raw_q;
+  }
+  if (slot < 0 || slot >= p.pages * p.page) return;
+  const int64_t pg = page_of(slot, p.page, p.by_page), row0 = pg * p.hk * p.page + (slot - pg * p.page);
+  // Run w of keys or values as a block's part.
+  auto put = [&](int w, const float* x, uint8_t* cache, uint8_t* scale) {
+    const int head = int(p.by_runs(unsigned(w))), e = (w - head * runs) * 8;
     uint32_t exponent;
     const uint32_t codes = cut_block<T>(x, &exponent);
-    const int64_t row = (pg * p.hk + kh) * p.page + off;
-    *reinterpret_cast<uint32_t*>((is_k ? p.k_cache : p.v_cache) + row * (p.d / 2) + e / 2) = codes;
-    if (e % kBlock4 == 0) (is_k ? p.k_scale : p.v_scale)[row * (p.d / kBlock4) + e / kBlock4] = uint8_t(exponent);
+    const int64_t row = row0 + int64_t(head) * p.page;
+    *reinterpret_cast<uint32_t*>(cache + row * (p.d / 2) + e / 2) = codes;
+    if (e % kBlock4 == 0) scale[row * (p.d / kBlock4) + e / kBlock4] = uint8_t(exponent);
+  };
+  for (int w = k0; w < k_runs; w += step) {
+    const int e = (w - int(p.by_runs(unsigned(w))) * runs) * 8;
+    if (w != k0) raw_k = load_run<WHOLE>(k + w * 8);
+    float x[8];
+    widen8<T>(raw_k, x);
+    if (e < p.rot) {
+      double y[8];
+      turn_run<T, INTER, WHOLE, double>(k + w * 8, e, p.rot, s_cos, s_sin, x, y);
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = round_odd(y[j]);
+        most = fmaxf(most, fabsf(x[j]));
+      }
+      if (most > 3e38f) {
+        // What is finite but past float32's range counts as its largest number.
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (fabs(y[j]) < __builtin_inf()) x[j] = float(fmin(fmax(y[j], -3.4028234663852886e38), 3.4028234663852886e38));
+      }
+    }
+    put(w, x, p.k_cache, p.k_scale);
+  }
+  for (int w = v0; w < k_runs; w += step) {
+    if (w != v0) raw_v = load_run<WHOLE>(v + w * 8);
+    float x[8];
+    widen8<T>(raw_v, x);
+    put(w, x, p.v_cache, p.v_scale);
   }
 }
 
-template <class T, bool INTER, bool WIDE>
+template <class T, bool INTER, bool WHOLE>
 hipError_t launch(const KvAppend4Params& p, hipStream_t stream) {
+  // As kv_append: few tokens are spread over more blocks, many tokens of few heads share one.
   const int64_t work = (int64_t(p.q ? p.hq : 0) + 2 * p.hk) * (p.d / 8);
   const unsigned y = unsigned(std::max<int64_t>(1, std::min<int64_t>(2048 / p.tokens, (work + 255) / 256)));
-  int threads = 256;
-  while (threads > 32 && threads / 2 >= work / 4 && p.tokens * (threads / 2) >= 256 * 256) threads /= 2;
-  const int64_t per = 256 / threads;
+  int shift = 8;
+  while (shift > 6 && (1 << shift) / 2 >= work / 4 && p.tokens * (1 << shift) / 2 >= 256 * 256) --shift;
+  const int64_t per = 256 >> shift;
   return launch_blocks((p.tokens + per - 1) / per, 256, [&](int64_t first, unsigned blocks) {
-    kv_append4_kernel<T, INTER, WIDE><<<dim3(blocks, y), dim3(256), size_t(per) * p.rot * 12, stream>>>(p, threads, first);
+    kv_append4_kernel<T, INTER, WHOLE><<<dim3(blocks, y), dim3(256), size_t(per) * p.rot * 12, stream>>>(p, shift, first);
   });
 }
 
@@ -199,9 +237,10 @@ bool aligned(const void* q, int64_t stride) { return reinterpret_cast<uintptr_t>
 
 template <class T>
 hipError_t launch_type(const KvAppend4Params& p, hipStream_t stream) {
-  const bool wide = (!p.q || aligned(p.q, p.q_stride)) && aligned(p.k, p.k_stride) && aligned(p.v, p.v_stride);
-  if (p.interleaved) return wide ? launch<T, true, true>(p, stream) : launch<T, true, false>(p, stream);
-  return wide ? launch<T, false, true>(p, stream) : launch<T, false, false>(p, stream);
+  const bool whole = (!p.q || aligned(p.q, p.q_stride)) && aligned(p.k, p.k_stride) && aligned(p.v, p.v_stride) &&
+                     p.rot % (p.interleaved ? 8 : 16) == 0;
+  if (p.interleaved) return whole ? launch<T, true, true>(p, stream) : launch<T, true, false>(p, stream);
+  return whole ? launch<T, false, true>(p, stream) : launch<T, false, false>(p, stream);
 }
 
 }  // namespace
