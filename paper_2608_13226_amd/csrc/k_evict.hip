@@ -169,7 +169,10 @@ __device__ __forceinline__ void copy_moves(const KvEvictParams& p, int threads, 
 // ---------------------------------------------------------------------------
 // Few rows: one launch.
 
-constexpr int kFewTokens = 16384;   // whose masses are in LDS
+// Longer sequences gain more by the chip's other compute units than several launches cost
+// (40 heads of 16384 tokens, 1639 kept: 43.8 us in one, 35.4 in five; 8192 tokens 33.8 and 34.6,
+// 4096 of which 2000 stay 34.7 and 39.0, 1702 of which 1638 do 12.8 and 28.4).
+constexpr int kFewTokens = 8192;    // whose masses are in LDS
 constexpr int kFewRows = 2048;      // that move: vacant places and `recent`
 using Top = Digits<4096, 2>;        // of the rank's highest 12 bits: most masses share an octave or two, and
 using Low = Digits<1024, 1>;        // additions to one address wait for each other; then two digits of 10
@@ -305,6 +308,7 @@ __global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
 
 constexpr int kBuckets = 1024;      // of the rank's highest 10 bits
 constexpr int kRest = 22 - 11;      // its other bits in two digits of 11
+constexpr int kSome = 16384;        // tokens of the bucket that a block has in LDS
 
 // Where the workspace holds what, for each (sequence, head), in 32-bit words.
 struct Lists {
@@ -340,6 +344,7 @@ struct Chunk {
   int kh, b, n, end, front, sink, want, j0, j1, per, w0, w1;
   const float* mass;
   uint32_t* ws;
+  float early[4];
 
   __device__ __forceinline__ Chunk(const KvEvictParams& p) : l(lists_of(p.keep, p.recent, p.max_length)) {
     kh = blockIdx.y;
@@ -358,17 +363,26 @@ struct Chunk {
     per = l.chunk / kWaves;
     w0 = min(j1, j0 + int(threadIdx.x) / kWave * per);
     w1 = min(j1, w0 + per);
+    // The first of them on their way before anything is waited for.
+    load(w0, early);
+  }
+
+  __device__ __forceinline__ void load(int t, float* m) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = t + e * kWave + int(threadIdx.x) % kWave;
+      m[e] = j < w1 ? mass[j] : 0.f;
+    }
   }
 
   // f(token, whether it is one, its mass) for this wave's tokens in order, 64 at a time and all
-  // lanes together; four loads are under way at once.
+  // lanes together.
   template <class F>
   __device__ __forceinline__ void each(F f) const {
     const int lane = threadIdx.x % kWave;
     for (int t = w0; t < w1; t += 4 * kWave) {
-      float m[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = t + e * kWave + lane < w1 ? mass[t + e * kWave + lane] : 0.f;
+      float m[4] = {early[0], early[1], early[2], early[3]};
+      if (t != w0) load(t, m);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (t + e * kWave < w1) f(t + e * kWave + lane, t + e * kWave + lane < w1, m[e]);
@@ -442,6 +456,7 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
 
 __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) {
   __shared__ Digits<2048, 2> s_low_digits;
+  __shared__ uint32_t s_some[kSome];
   __shared__ int s_equal[64], s_low[64], s_high[64], s_equal_low[64];
   __shared__ int s_wave[4][kWaves];
   const Chunk c(p);
@@ -456,64 +471,85 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     }
     return;
   }
-  const uint32_t* stats = c.ws + c.l.stats;
+  // Lane k has chunk k.
+  const int k_mine = min(lane, c.l.chunks - 1);
+  int ties = 0, count = 0, above_low = 0, above_high = 0, before = 0;
   uint32_t border = 0u;
-  int ties = 0;
   if (c.want > 0) {
+    const uint32_t* stats = c.ws + c.l.stats + k_mine * 4;
+    count = lane < c.l.chunks ? int(stats[0]) : 0;
+    above_low = int(stats[1]);
+    above_high = int(stats[2]);
     const uint32_t bucket = stats[3];
     ties = int(c.ws[c.l.ties]);
+    // The tokens in the bucket, in LDS where it has room for all.
+    const int upto = wave_upto(count);
+    before = upto - count;
+    const bool fits = __builtin_amdgcn_readlane(upto, kWave - 1) <= kSome;
+    if (fits) {
+      for (int k = wave; k < c.l.chunks; k += kWaves) {
+        const int n = __builtin_amdgcn_readlane(count, k), at = __builtin_amdgcn_readlane(before, k);
+        const uint32_t* some = c.ws + c.l.some + int64_t(k) * c.l.chunk;
+#pragma unroll 4
+        for (int i = lane; i < n; i += kWave) s_some[at + i] = some[i];
+      }
+    }
+    // f(chunk, its tokens in the bucket, how many): a wave takes every 16th chunk.
+    auto each_some = [&](auto f) {
+      for (int k = wave; k < c.l.chunks; k += kWaves) {
+        const int n = __builtin_amdgcn_readlane(count, k);
+        if (fits) f(k, s_some + __builtin_amdgcn_readlane(before, k), n);
+        else f(k, c.ws + c.l.some + int64_t(k) * c.l.chunk, n);
+      }
+    };
     uint32_t low = 0u;
 #pragma unroll 1
     for (int shift = kRest; shift >= 0; shift -= kRest) {
       s_low_digits.clear();
       lds_sync();
-      // A wave takes every 16th chunk's tokens of the bucket.
-      for (int k = wave; k < c.l.chunks; k += kWaves) {
-        const int count = int(stats[k * 4]);
-        const uint32_t* some = c.ws + c.l.some + int64_t(k) * c.l.chunk;
+      each_some([&](int, const uint32_t* some, int n) {
 #pragma unroll 4
-        for (int i = lane; i < count; i += kWave) {
+        for (int i = lane; i < n; i += kWave) {
           const uint32_t r = some[i] & 0x3fffffu;
           if (shift == kRest || r >> kRest == low >> kRest) s_low_digits.add(r >> shift & 2047u);
         }
-      }
+      });
       lds_sync();
       low |= s_low_digits.find(ties) << shift;
     }
     border = bucket << 22 | low;
     // Each chunk's tokens at the border and above it.
-    for (int k = wave; k < c.l.chunks; k += kWaves) {
-      const int count = int(stats[k * 4]);
-      const uint32_t* some = c.ws + c.l.some + int64_t(k) * c.l.chunk;
-      int equal = 0, equal_low = 0, above_low = int(stats[k * 4 + 1]), above_high = int(stats[k * 4 + 2]);
-      for (int i0 = 0; i0 < count; i0 += kWave) {
-        const bool here = i0 + lane < count;
+    each_some([&](int k, const uint32_t* some, int n) {
+      int equal = 0, equal_low = 0, more_low = 0, more_high = 0;
+      for (int i0 = 0; i0 < n; i0 += kWave) {
+        const bool here = i0 + lane < n;
         const uint32_t v = here ? some[i0 + lane] : 0u, r = v & 0x3fffffu;
         const bool below = v >> 31 != 0u;
         equal += __popcll(__ballot(here && r == low));
         equal_low += __popcll(__ballot(here && r == low && below));
-        above_low += __popcll(__ballot(here && r > low && below));
-        above_high += __popcll(__ballot(here && r > low && !below));
+        more_low += __popcll(__ballot(here && r > low && below));
+        more_high += __popcll(__ballot(here && r > low && !below));
       }
       if (lane == 0) {
         s_equal[k] = equal;
         s_equal_low[k] = equal_low;
-        s_low[k] = above_low;
-        s_high[k] = above_high;
+        s_low[k] = more_low;
+        s_high[k] = more_high;
       }
-    }
+    });
   } else if (tid < c.l.chunks) {
     s_equal[tid] = s_equal_low[tid] = s_low[tid] = s_high[tid] = 0;
   }
   lds_sync();
-  // Up to this chunk: ties, vacant places, movers.  And all vacant places.  Lane k has chunk k.
+  // Up to this chunk: ties, vacant places, movers.  And all vacant places.
   int tie0, gap0, go0, gaps;
   {
-    const int k = min(lane, c.l.chunks - 1), a = k * c.l.chunk, z = min(c.front, min(c.end, a + c.l.chunk));
+    const int k = k_mine, a = k * c.l.chunk, z = min(c.front, min(c.end, a + c.l.chunk));
     const int equal = lane < c.l.chunks ? s_equal[k] : 0, before = wave_upto(equal) - equal;
     const int taken = min(max(ties - before, 0), equal), taken_low = min(taken, s_equal_low[k]);
     const int sinks = min(max(c.sink - a, 0), c.l.chunk);
-    const int gap = lane < c.l.chunks ? max(z - a, 0) - (sinks + s_low[k] + taken_low) : 0, go = s_high[k] + taken - taken_low;
+    const int gap = lane < c.l.chunks ? max(z - a, 0) - (sinks + above_low + s_low[k] + taken_low) : 0;
+    const int go = above_high + s_high[k] + taken - taken_low;
     const int gaps_upto = wave_upto(gap), go_upto = wave_upto(go), me = int(blockIdx.x);
     tie0 = __builtin_amdgcn_readlane(before, me);
     gap0 = __builtin_amdgcn_readlane(gaps_upto - gap, me);
@@ -521,20 +557,20 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     gaps = __builtin_amdgcn_readlane(gaps_upto, kWave - 1);
   }
   // Then up to this wave, from each wave's tokens at the border and above it.
-  int equal = 0, equal_low = 0, above_low = 0, above_high = 0;
+  int equal = 0, equal_low = 0, more_low = 0, more_high = 0;
   c.each([&](int j, bool here, float m) {
     const uint32_t r = rank_of(m);
     const bool inner = here && c.want > 0 && j >= c.sink, above = here && (j < c.sink || (inner && r > border));
     equal += __popcll(__ballot(inner && r == border));
     equal_low += __popcll(__ballot(inner && r == border && j < c.front));
-    above_low += __popcll(__ballot(above && j < c.front));
-    above_high += __popcll(__ballot(above && j >= c.front));
+    more_low += __popcll(__ballot(above && j < c.front));
+    more_high += __popcll(__ballot(above && j >= c.front));
   });
   if (lane == 0) {
     s_wave[0][wave] = equal;
     s_wave[1][wave] = equal_low;
-    s_wave[2][wave] = above_low;
-    s_wave[3][wave] = above_high;
+    s_wave[2][wave] = more_low;
+    s_wave[3][wave] = more_high;
   }
   lds_sync();
   for (int w = 0; w < wave; ++w) {
