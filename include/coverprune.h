@@ -635,7 +635,7 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
  * NaN: the byte is 255 (and the codes 0).
  *
  *   q, k, v, dtype, positions, slots, inv_freq, rot, interleaved, magnitude, q_out
- *              as for coverprune_kv_append, but q_out is not q; d a multiple of 32,
+ *              as for coverprune_kv_append, but q_out overlaps none of q, k, v; d a multiple of 32,
  *              at most 4096.  Elements go eight at a time where q, k, v and their
  *              strides are 16-byte aligned.
  *   k_cache, v_cache  [pages, hk, page_size, d / 2] bytes: two codes each, the
@@ -719,8 +719,9 @@ cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t
  *   kept       [batch, hk, keep] int32 output: which token is now at each place, -1
  *              from the new length on
  *   mass_out   [batch, hk, mass_span] float output, may be mass: the masses in the new
- *              order, 0 from the new length on
- *   lengths_out  [batch] int32 output, not lengths: the new lengths, at most keep
+ *              order, 0 from the new length on (otherwise without overlap)
+ *   lengths_out  [batch] int32 output that does not overlap lengths: the new lengths, at
+ *              most keep
  *   workspace  coverprune_kv_evict_workspace bytes
  */
 size_t coverprune_kv_evict_workspace(int64_t batch, int64_t hk, int64_t keep, int64_t recent, int64_t max_length);

@@ -801,6 +801,8 @@ static cp_status attend(bool mass, cp::AttendParams& p, cp_dtype dtype, int64_t 
   if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
   if ((st = check_pages(p.pages, page_size, hk, width, p.max_length)) != CP_OK) return st;
   if (!std::isfinite(p.scale)) return fail(CP_ERR_INVALID_ARG, "scale must be finite");
+  if ((mass || held == CP_E2M1) && batch > 0 && !cp::attend_fits(batch, hq, hk, d, p.max_length, window, mass, held == CP_E2M1))
+    return fail(CP_ERR_UNSUPPORTED, "batch = %lld sequences of %lld heads are too many for one call", (long long)batch, (long long)hq);
   if (mass && (p.mass_span < p.max_length || p.mass_span >= int64_t(1) << 31))
     return fail(CP_ERR_INVALID_ARG, "mass_span = %lld outside [max_length, 2^31)", (long long)p.mass_span);
   if (batch == 0) return ok();
@@ -901,6 +903,12 @@ cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t
   return attend(true, p, dtype, batch, hq, hk, d, cache_dtype, page_size, width, window, workspace_bytes, stream);
 }
 
+// Whether `n` bytes from a on and `m` from b on share any.
+static bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + uintptr_t(m) && y < x + uintptr_t(n);
+}
+
 cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
                                 const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
@@ -922,7 +930,10 @@ cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, 
   if (!k || !v || !positions || !slots || !k_cache || !v_cache || !k_scale || !v_scale || (rot && !inv_freq) || (q && !q_out))
     return fail(CP_ERR_INVALID_ARG,
                 "k, v, positions, slots, inv_freq, k_cache, v_cache, k_scale, v_scale and (with q) q_out must be non-NULL");
-  if (q && q == q_out) return fail(CP_ERR_INVALID_ARG, "q_out must not be q");
+  if (q && (overlap(q_out, tokens * hq * d * 2, q, ((tokens - 1) * q_stride + hq * d) * 2) ||
+            overlap(q_out, tokens * hq * d * 2, k, ((tokens - 1) * k_stride + hk * d) * 2) ||
+            overlap(q_out, tokens * hq * d * 2, v, ((tokens - 1) * v_stride + hk * d) * 2)))
+    return fail(CP_ERR_INVALID_ARG, "q_out must not overlap q, k or v");
   if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q_out))
     return fail(CP_ERR_INVALID_ARG, "k_cache, v_cache and q_out must be 16-byte aligned");
 
@@ -1037,7 +1048,9 @@ cp_status coverprune_kv_evict(void* k_cache, void* v_cache, cp_dtype cache_dtype
   if (!k_cache || !v_cache || !table || !lengths || !mass || !kept || !mass_out || !lengths_out || (four && (!k_scale || !v_scale)))
     return fail(CP_ERR_INVALID_ARG,
                 "k_cache, v_cache, table, lengths, mass, kept, mass_out, lengths_out and (4 bits) k_scale and v_scale must be non-NULL");
-  if (lengths_out == lengths) return fail(CP_ERR_INVALID_ARG, "lengths_out must not be lengths");
+  if (overlap(lengths_out, batch * 4, lengths, batch * 4)) return fail(CP_ERR_INVALID_ARG, "lengths_out must not overlap lengths");
+  if (mass_out != mass && overlap(mass_out, batch * hk * mass_span * 4, mass, batch * hk * mass_span * 4))
+    return fail(CP_ERR_INVALID_ARG, "mass_out must be mass or not overlap it");
   if (!aligned16(k_cache) || !aligned16(v_cache)) return fail(CP_ERR_INVALID_ARG, "k_cache and v_cache must be 16-byte aligned");
   if ((st = check_workspace(workspace, workspace_bytes, cp::evict_workspace_bytes(batch, hk, keep, recent, max_length))) != CP_OK)
     return st;

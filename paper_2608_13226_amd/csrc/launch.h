@@ -344,6 +344,8 @@ struct AttendParams {
 };
 // 0 where one launch writes the result.
 size_t attend_workspace_bytes(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass, bool four);
+// Whether HIP launches as many blocks as the join of the runs takes.
+bool attend_fits(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass, bool four);
 hipError_t launch_attend(const AttendParams& p, hipStream_t stream);
 hipError_t launch_attend4(const AttendParams& p, hipStream_t stream);
 hipError_t launch_attend_mass(const AttendParams& p, hipStream_t stream);
