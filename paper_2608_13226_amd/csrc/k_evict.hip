@@ -12,9 +12,9 @@
 // counts of them; of those at the last rank the earlier.  The order of tokens comes
 // from counts as well, so nothing depends on the order of atomics.
 //
-//   evict_few    where few rows move, all of it by a block a (sequence, head), the
-//                masses in LDS
-//   otherwise, with a sequence's tokens in up to 64 chunks:
+//   evict_one    up to 16384 tokens: a block a (sequence, head) selects, the ranks in LDS;
+//                where few rows move, it moves them too, and one launch does it all
+//   longer sequences have their tokens in up to 64 chunks:
 //   evict_count  a chunk's counts of the rank's highest 10 bits
 //   evict_bucket the value of those at which the rank wanted lies; a chunk's tokens that
 //                have it, its counts of those above
@@ -166,150 +166,10 @@ __device__ __forceinline__ void copy_moves(const KvEvictParams& p, int threads, 
     copy_rows<IN_ORDER, U>(p, p.k_exps, p.v_exps, p.exp_bytes, threads, moves, first, step, places);
 }
 
-// ---------------------------------------------------------------------------
-// Few rows: one launch.
-
-// Longer sequences gain more by the chip's other compute units than several launches cost
-// (40 heads of 16384 tokens, 1639 kept: 43.8 us in one, 35.4 in five; 8192 tokens 33.8 and 34.6,
-// 4096 of which 2000 stay 34.7 and 39.0, 1702 of which 1638 do 12.8 and 28.4).
-constexpr int kFewTokens = 8192;    // whose masses are in LDS
-constexpr int kFewRows = 2048;      // that move: vacant places and `recent`
-using Top = Digits<4096, 2>;        // of the rank's highest 12 bits: most masses share an octave or two, and
-using Low = Digits<1024, 1>;        // additions to one address wait for each other; then two digits of 10
-
-template <class U>
-__global__ __launch_bounds__(kSelect) void evict_few_kernel(KvEvictParams p) {
-  extern __shared__ float s_mass[];                         // [max_length]
-  __shared__ Top s_top;
-  __shared__ Low s_low[2];
-  __shared__ uint32_t s_to[kFewRows], s_from[kFewRows];     // tokens, then their rows
-  __shared__ int s_ties[kWaves], s_both[kWaves];
-  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink), m = min(n, keep);
-  const int64_t head = int64_t(b) * p.hk + kh;
-  const float* mass = p.mass + head * p.span;
-  float* out = p.mass_out + head * p.span;
-  int32_t* kept = p.kept + head * p.keep;
-  if (kh == 0 && tid == 0) p.lengths_out[b] = m;
-  if (n <= keep) {
-    for (int64_t j = tid; j < keep; j += kSelect) kept[j] = j < n ? int(j) : -1;
-    for (int64_t j = tid; j < p.span; j += kSelect) out[j] = j < n ? mass[j] : 0.f;
-    return;
-  }
-  const int end = n - recent, front = keep - recent, want = front - sink;
-  s_top.clear();
-  s_low[0].clear();
-  s_low[1].clear();
-#pragma unroll 16
-  for (int j = tid; j < n; j += kSelect) s_mass[j] = mass[j];
-  lds_sync();
-  uint32_t border = 0u;
-  int ties = want;
-  if (want > 0) {
-#pragma unroll 4
-    for (int j = sink + tid; j < end; j += kSelect) s_top.add(rank_of(s_mass[j]) >> 20);
-    lds_sync();
-    border = s_top.find(ties) << 20;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int shift = 10 - 10 * i;
-#pragma unroll 4
-      for (int j = sink + tid; j < end; j += kSelect) {
-        const uint32_t r = rank_of(s_mass[j]);
-        if ((r ^ border) >> (shift + 10) == 0u) s_low[i].add(r >> shift & 1023u);
-      }
-      lds_sync();
-      border |= s_low[i].find(ties) << shift;
-    }
-  }
-  // Each wave has consecutive tokens: how many are at the border, then how many places
-  // fall vacant below the front and how many tokens from it on stay.
-  const int run = (end + kSelect - 1) / kSelect * kWave, j0 = wave * run, j1 = min(end, j0 + run);
-  int equal = 0;
-  for (int j = j0 + lane; j < j1; j += kWave) equal += __popcll(__ballot(want > 0 && j >= sink && rank_of(s_mass[j]) == border));
-  if (lane == 0) s_ties[wave] = j0 < j1 ? equal : 0;
-  lds_sync();
-  int tie0 = 0;
-  for (int w = 0; w < wave; ++w) tie0 += s_ties[w];
-  // Token j (every lane of the wave comes along): whether it stays; `seen` counts ties.
-  auto stays = [&](int j, int& seen) {
-    const bool here = j < j1;
-    const uint32_t r = here ? rank_of(s_mass[j]) : 0u;
-    const bool tie = here && want > 0 && j >= sink && r == border;
-    const unsigned long long all = __ballot(tie);
-    const bool yes = here && (j < sink || (want > 0 && (r > border || (tie && seen + lanes_below(all) < ties))));
-    seen += __popcll(all);
-    return yes;
-  };
-  int seen = tie0, gaps = 0, goes = 0;
-  for (int t = j0; t < j1; t += kWave) {
-    const int j = t + lane;
-    const bool yes = stays(j, seen);
-    gaps += __popcll(__ballot(j < j1 && !yes && j < front));
-    goes += __popcll(__ballot(yes && j >= front));
-  }
-  if (lane == 0) s_both[wave] = gaps | goes << 16;
-  lds_sync();
-  int both = 0, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    const int v = s_both[w];
-    if (w < wave) both += v;
-    total += v;
-  }
-  total &= 0xffff;
-  int gap_at = both & 0xffff, go_at = both >> 16;
-  seen = tie0;
-  for (int t = j0; t < j1; t += kWave) {
-    const int j = t + lane;
-    const bool yes = stays(j, seen), gap = j < j1 && !yes && j < front, go = yes && j >= front;
-    const unsigned long long all_gaps = __ballot(gap), all_go = __ballot(go);
-    if (yes && !go) {
-      kept[j] = j;
-      out[j] = s_mass[j];
-    }
-    if (gap) s_to[gap_at + lanes_below(all_gaps)] = j;
-    if (go) s_from[go_at + lanes_below(all_go)] = j;
-    gap_at += __popcll(all_gaps);
-    go_at += __popcll(all_go);
-  }
-  const int moves = total + recent;
-  for (int i = total + tid; i < moves; i += kSelect) {
-    s_to[i] = front + i - total;
-    s_from[i] = end + i - total;
-  }
-  lds_sync();
-  for (int i = tid; i < moves; i += kSelect) {
-    const int to = s_to[i], from = s_from[i];
-    kept[to] = from;
-    out[to] = s_mass[from];
-  }
-  for (int64_t j = m + tid; j < p.span; j += kSelect) out[j] = 0.f;
-  const Place place = {p, b, kh};
-  for (int i = tid; i < moves; i += kSelect) {
-    // (Each thread's own moves, so far.)
-    s_to[i] = place.row(s_to[i]);
-    s_from[i] = place.row(s_from[i]);
-  }
-  lds_sync();
-  copy_moves<false, U>(p, kSelect, total, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
-    *to = s_to[i];
-    *from = s_from[i];
-  });
-  if (recent == 0) return;
-  __syncthreads();
-  copy_moves<true, U>(p, kSelect, recent, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
-    *to = s_to[total + i];
-    *from = s_from[total + i];
-  });
-}
-
-// ---------------------------------------------------------------------------
-// Many rows.
+// The mass of a rank (a NaN for NaN, 0 for -0).
+__device__ __forceinline__ float mass_of(uint32_t r) { return __uint_as_float(r == 0u ? 0x7fc00000u : r & 0x80000000u ? r ^ 0x80000000u : ~r); }
 
 constexpr int kBuckets = 1024;      // of the rank's highest 10 bits
-constexpr int kRest = 22 - 11;      // its other bits in two digits of 11
-constexpr int kSome = 16384;        // tokens of the bucket that a block has in LDS
-
 // Where the workspace holds what, for each (sequence, head), in 32-bit words.
 struct Lists {
   int chunks, chunk;                // tokens a chunk, a multiple of kSelect
@@ -336,6 +196,194 @@ __host__ __device__ inline Lists lists_of(int64_t keep, int64_t recent, int64_t 
   l.stride = l.gaps + 1;
   return l;
 }
+
+// ---------------------------------------------------------------------------
+// Up to 16384 tokens: selected by one block.
+
+// A sequence's tokens are in one block's LDS up to here: 7.3 us for 64 tokens, 0.8 for each 1024
+// more.  In chunks over the chip it is the launches' time (40 heads of 16384 tokens, 1639 kept: 32.2
+// us with three launches and 35.4 with five; a sequence of 16384 of 4 heads 26.4 and 28.5).
+constexpr int kOneTokens = 16384, kWords = kOneTokens / kWave;
+// As many moves are made by the same block, which has one compute unit's share of the memory's rate:
+// vacant places and `recent` (32 heads of 4096 tokens, 1000 kept: 24.7 us; with two more launches
+// and 2000 kept 28.2, where one took 34.7).
+constexpr int kFewRows = 1024;
+using Top = Digits<4096, 2>;        // of the rank's highest 12 bits: most masses share an octave or two, and
+using Low = Digits<1024, 1>;        // additions to one address wait for each other; then two digits of 10
+
+// FEW: the block moves the rows as well; otherwise it leaves lists for evict_move.
+template <class U, bool FEW>
+__global__ __launch_bounds__(kSelect) void evict_one_kernel(KvEvictParams p) {
+  extern __shared__ uint32_t s_rank[];                      // [max_length]
+  __shared__ Top s_top;
+  __shared__ Low s_low[2];
+  // Of 64 tokens each: who is above the border, at it, stays; gaps and movers before them.
+  __shared__ uint64_t s_above[kWords], s_equal[kWords];
+  __shared__ int s_at[kWords], s_part[2][kWaves];
+  __shared__ uint32_t s_to[FEW ? kFewRows : 1], s_from[FEW ? kFewRows : 1];     // tokens, then their rows
+  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink), m = min(n, keep);
+  const int64_t head = int64_t(b) * p.hk + kh;
+  const float* mass = p.mass + head * p.span;
+  int32_t* kept = p.kept + head * p.keep;
+  const Lists l = lists_of(p.keep, p.recent, p.max_length);
+  uint32_t* ws = static_cast<uint32_t*>(p.workspace) + (FEW ? 0 : head * l.stride);
+  // The new masses: in place, or for evict_move.
+  float* out = FEW ? p.mass_out + head * p.span : reinterpret_cast<float*>(ws + l.mass);
+  if (FEW && kh == 0 && tid == 0) p.lengths_out[b] = m;
+  if (n <= keep) {
+    for (int64_t j = tid; j < keep; j += kSelect) kept[j] = j < n ? int(j) : -1;
+    for (int64_t j = tid; j < (FEW ? p.span : n); j += kSelect) out[j] = j < n ? mass[j] : 0.f;
+    return;
+  }
+  const int end = n - recent, front = keep - recent, want = front - sink;
+  s_top.clear();
+  s_low[0].clear();
+  s_low[1].clear();
+  lds_sync();
+  // Eight loads under way at once.
+  for (int j0 = tid; j0 < n; j0 += 8 * kSelect) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = mass[min(j0 + e * kSelect, n - 1)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = j0 + e * kSelect;
+      const uint32_t r = rank_of(v[e]);
+      if (j < n) s_rank[j] = r;
+      if (j >= sink && j < end) s_top.add(r >> 20);
+    }
+  }
+  lds_sync();
+  uint32_t border = 0u;
+  int ties = want;
+  if (want > 0) {
+    border = s_top.find(ties) << 20;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int shift = 10 - 10 * i;
+#pragma unroll 4
+      for (int j = sink + tid; j < end; j += kSelect) {
+        const uint32_t r = s_rank[j];
+        if ((r ^ border) >> (shift + 10) == 0u) s_low[i].add(r >> shift & 1023u);
+      }
+      lds_sync();
+      border |= s_low[i].find(ties) << shift;
+    }
+  }
+  const int words = (end + kWave - 1) / kWave;
+  for (int w = wave; w < words; w += kWaves) {
+    const int j = w * kWave + lane;
+    const uint32_t r = s_rank[min(j, n - 1)];
+    const bool here = j < end, inner = here && want > 0 && j >= sink;
+    const unsigned long long above = __ballot((here && j < sink) || (inner && r > border)), equal = __ballot(inner && r == border);
+    if (lane == 0) {
+      s_above[w] = above;
+      s_equal[w] = equal;
+    }
+  }
+  lds_sync();
+  // A thread a word: the first ties stay too, then gaps below the front and movers from it on, both counts in one number.
+  static_assert(kWords <= kSelect, "a thread has one word");
+  const uint64_t equal = tid < words ? s_equal[tid] : 0u;
+  const int equal_upto = wave_upto(__popcll(equal));
+  if (lane == kWave - 1) s_part[0][wave] = equal_upto;
+  lds_sync();
+  int left = ties - (equal_upto - __popcll(equal));
+  for (int w = 0; w < wave; ++w) left -= s_part[0][w];
+  uint64_t over = equal;                                    // ties that leave
+  for (int i = 0; i < left && over != 0u; ++i) over &= over - 1;
+  uint64_t stays = 0u;
+  int count = 0;
+  if (tid < words) {
+    auto first = [&](int upto) {                            // the word's tokens below `upto`
+      const int k = min(max(upto - tid * kWave, 0), kWave);
+      return k == kWave ? ~uint64_t(0) : (uint64_t(1) << k) - 1;
+    };
+    stays = s_above[tid] | (equal ^ over);
+    count = __popcll(first(end) & first(front) & ~stays) | __popcll(stays & ~first(front)) << 16;
+  }
+  const int upto = wave_upto(count);
+  if (lane == kWave - 1) s_part[1][wave] = upto;
+  lds_sync();
+  int before = upto - count, total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    const int v = s_part[1][w];
+    if (w < wave) before += v;
+    total += v;
+  }
+  total &= 0xffff;
+  if (tid < words) {
+    s_above[tid] = stays;
+    s_at[tid] = before;
+  }
+  lds_sync();
+  int *vacant = reinterpret_cast<int*>(ws + l.vacant), *movers = reinterpret_cast<int*>(ws + l.movers);
+  float* mover_mass = reinterpret_cast<float*>(ws + l.mover_mass);
+  for (int w = wave; w < words; w += kWaves) {
+    const int j = w * kWave + lane, at = s_at[w];
+    const bool yes = s_above[w] >> lane & 1u, gap = j < min(end, front) && !yes, go = yes && j >= front;
+    const int gap_at = (at & 0xffff) + lanes_below(__ballot(gap)), go_at = (at >> 16) + lanes_below(__ballot(go));
+    const uint32_t r = s_rank[min(j, n - 1)];
+    if (yes && !go) {
+      kept[j] = j;
+      out[j] = mass_of(r);
+    }
+    if constexpr (FEW) {
+      if (gap) s_to[gap_at] = j;
+      if (go) s_from[go_at] = j;
+    } else {
+      if (gap) {
+        kept[j] = -1;               // until evict_move fills it
+        vacant[gap_at] = j;
+      }
+      if (go) {
+        movers[go_at] = j;
+        mover_mass[go_at] = mass_of(r);
+      }
+    }
+  }
+  if constexpr (!FEW) {
+    for (int i = tid; i < recent; i += kSelect) {
+      kept[front + i] = end + i;
+      out[front + i] = mass_of(s_rank[end + i]);
+    }
+    if (tid == 0) ws[l.gaps] = uint32_t(total);
+    return;
+  }
+  const int moves = total + recent;
+  for (int i = total + tid; i < moves; i += kSelect) {
+    s_to[i] = front + i - total;
+    s_from[i] = end + i - total;
+  }
+  lds_sync();
+  const Place place = {p, b, kh};
+  for (int i = tid; i < moves; i += kSelect) {
+    const int to = s_to[i], from = s_from[i];
+    kept[to] = from;
+    out[to] = mass_of(s_rank[from]);
+    s_to[i] = place.row(to);
+    s_from[i] = place.row(from);
+  }
+  for (int64_t j = m + tid; j < p.span; j += kSelect) out[j] = 0.f;
+  lds_sync();
+  copy_moves<false, U>(p, kSelect, total, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
+    *to = s_to[i];
+    *from = s_from[i];
+  });
+  if (recent == 0) return;
+  __syncthreads();
+  copy_moves<true, U>(p, kSelect, recent, 0, 1, [&](int i, uint32_t* to, uint32_t* from) {
+    *to = s_to[total + i];
+    *from = s_from[total + i];
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Longer sequences.
+
+constexpr int kRest = 22 - 11;      // its other bits in two digits of 11
+constexpr int kSome = 16384;        // tokens of the bucket that a block has in LDS
 
 // What the blocks of a (sequence, head) share.
 struct Chunk {
@@ -664,23 +712,28 @@ __global__ __launch_bounds__(kSelect) void evict_shift_kernel(KvEvictParams p) {
 
 // Whether one launch does it all.
 bool few_rows(int64_t keep, int64_t recent, int64_t max_length) {
-  return max_length <= keep || (max_length <= kFewTokens && lists_of(keep, recent, max_length).places + recent <= kFewRows);
+  return max_length <= keep || (max_length <= kOneTokens && lists_of(keep, recent, max_length).places + recent <= kFewRows);
 }
 
 template <class U>
 hipError_t launch(const KvEvictParams& p, hipStream_t stream) {
-  if (few_rows(p.keep, p.recent, p.max_length)) {
-    const size_t ranks = p.max_length <= p.keep ? 0 : size_t(p.max_length) * sizeof(uint32_t);
-    evict_few_kernel<U><<<dim3(unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), ranks, stream>>>(p);
+  const bool few = few_rows(p.keep, p.recent, p.max_length);
+  const size_t ranks = p.max_length <= p.keep ? 0 : size_t(p.max_length) * sizeof(uint32_t);
+  if (few) {
+    evict_one_kernel<U, true><<<dim3(unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), ranks, stream>>>(p);
     return hipGetLastError();
   }
   const Lists l = lists_of(p.keep, p.recent, p.max_length);
   const dim3 grid(unsigned(l.chunks), unsigned(p.hk), unsigned(p.batch));
-  if (p.keep > p.recent + p.sink) {
-    evict_count_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
-    evict_bucket_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
+  if (p.max_length <= kOneTokens) {
+    evict_one_kernel<U, false><<<dim3(unsigned(p.hk), unsigned(p.batch)), dim3(kSelect), ranks, stream>>>(p);
+  } else {
+    if (p.keep > p.recent + p.sink) {
+      evict_count_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
+      evict_bucket_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
+    }
+    evict_border_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
   }
-  evict_border_kernel<<<grid, dim3(kSelect), 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // Enough blocks for four moves a thread, or 2048 masses a block.
