@@ -120,6 +120,19 @@ def test_mass(lengths, hq, hk, d, page, t, held):
     assert torch.equal(out, same[0]) and torch.equal(lse, same[1])
 
 
+@pytest.mark.parametrize("held", ["same", "e2m1"])
+@pytest.mark.parametrize("lengths,hq,hk,d,page,t", [
+    ([512, 40], 16, 1, 256, 16, BF), ([500], 8, 1, 256, 50, F16), ([1024 - 25 * i for i in range(40)], 4, 2, 64, 16, BF),
+    ([1000 - 10 * i for i in range(33)], 32, 2, 128, 32, F16), ([768, 760, 1], 8, 8, 128, 16, BF), ([769], 16, 1, 96, 16, F16),
+    ([700], 17, 1, 64, 64, BF), ([300], 100, 2, 128, 16, BF)])
+def test_mass_where_one_block_has_all_and_where_not_quite(lengths, hq, hk, d, page, t, held):
+    """Scores that fit a block's LDS, or just do not; more heads than a block has columns."""
+    print(f"mass {len(lengths)} sequences, heads={hq}/{hk} d={d} {t} {held}", flush=True)
+    a = _data(lengths, hq, hk, d, page, t, held)
+    _check_mass(a)
+    _check_mass(a, window=200, span=1100)
+
+
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("window", [1, 31, 33, 500, 5000])
 def test_windows(window, page):

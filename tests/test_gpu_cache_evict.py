@@ -149,9 +149,10 @@ def test_pages_outside_the_cache_are_clamped():
 @pytest.mark.parametrize("lengths,hk,keep,recent,sink,ties", [
     ([20000, 16384, 2500, 16000], 2, 2500, 100, 5, False), ([40000, 39000], 2, 20000, 15000, 64, True),
     ([16385], 1, 4000, 0, 0, True), ([30000, 12], 1, 29000, 29000, 0, False), ([30000], 2, 5000, 4000, 1000, False),
+    ([16384, 16383], 2, 16000, 128, 4, True), ([16384], 1, 16383, 0, 0, False), ([16385, 9], 1, 16384, 1, 0, True),
     ([300000, 299999], 1, 150000, 100, 10, True), ([5000] * 4, 3, 2400, 300, 0, False), ([16384] * 2, 1, 8000, 8000, 0, False)])
 def test_many_rows(lengths, hk, keep, recent, sink, ties):
-    """Those that go in several launches: chunks, boundaries inside them, sequences that are short enough beside them."""
+    """Those that go in several launches, or nearly: chunks, boundaries inside them, sequences that are short enough beside them."""
     for held in ("e2m1", "bf16"):
         a = _data(lengths, hk, 64, 50, held, ties=ties)
         _check({x: y.clone() if y is not None else None for x, y in a.items()}, keep, recent, sink)
