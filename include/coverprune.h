@@ -686,7 +686,8 @@ cp_status coverprune_paged_attention4(const void* q, cp_dtype dtype, int64_t bat
  *
  *   cache_dtype  dtype, CP_E4M3 or CP_E2M1; k_scale and v_scale go with it as for
  *              coverprune_kv_gather
- *   mass       [batch, hk, mass_span] float, mass_span >= max_length
+ *   mass       [batch, hk, mass_span] float, mass_span >= max_length; aligned as a float
+ *              is, so that sequences of any span can be part of a larger array
  *   workspace  coverprune_paged_attention_mass_workspace bytes, 4 * batch * hq *
  *              max_length of them for the scores
  */
@@ -714,7 +715,8 @@ cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t
  *   k_scale, v_scale  CP_E2M1: the exponents, which move with their rows; otherwise NULL
  *   table, lengths, max_length  as for coverprune_paged_attention.  Pages that two
  *              sequences share are the caller's error.
- *   mass       [batch, hk, mass_span] float, mass_span >= max_length
+ *   mass       [batch, hk, mass_span] float, mass_span >= max_length (mass, mass_out, kept and
+ *              lengths_out aligned as their elements are)
  *   keep       1 <= keep < 2^31; recent >= 0, sink >= 0, recent + sink <= keep
  *   kept       [batch, hk, keep] int32 output: which token is now at each place, -1
  *              from the new length on

@@ -810,8 +810,8 @@ static cp_status attend(bool mass, cp::AttendParams& p, cp_dtype dtype, int64_t 
     return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, table, lengths and out must be non-NULL");
   if (held == CP_E2M1 && (!p.k_exps || !p.v_exps)) return fail(CP_ERR_INVALID_ARG, "k_scale and v_scale must be non-NULL with a 4-bit cache");
   if (mass && !p.mass) return fail(CP_ERR_INVALID_ARG, "mass must be non-NULL");
-  if (!aligned16(p.q) || !aligned16(p.k_cache) || !aligned16(p.v_cache) || !aligned16(p.out) || (mass && !aligned16(p.mass)))
-    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache, out and mass must be 16-byte aligned");
+  if (!aligned16(p.q) || !aligned16(p.k_cache) || !aligned16(p.v_cache) || !aligned16(p.out))
+    return fail(CP_ERR_INVALID_ARG, "q, k_cache, v_cache and out must be 16-byte aligned");
   if ((st = check_workspace(p.workspace, workspace_bytes, cp::attend_workspace_bytes(batch, hq, hk, d, p.max_length, window, mass, held == CP_E2M1))) != CP_OK)
     return st;
   p.batch = int(batch);

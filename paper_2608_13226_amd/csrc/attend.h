@@ -279,7 +279,7 @@ __device__ __forceinline__ void keep_loads_here() { asm volatile("" ::: "memory"
 template <class T, Held C, int D, int W, bool UNI, bool MASS>
 __global__ __launch_bounds__(64 * W, W == 16 ? 1 : 2) void attend_kernel(AttendParams p, int tiles_per_run, int runs, float* part_o,
                                                            float* part_ml, float* scores, bool whole) {
-  extern __shared__ float s_x[];                // MASS, whole: the scores [heads][tokens]
+  extern __shared__ __attribute__((aligned(16))) float s_x[];   // MASS, whole: the scores [heads][tokens]
   constexpr int kSteps = D / 32;
   using L = Dims<D>;
   __shared__ float s_o[W][16][D + 4];

@@ -109,7 +109,7 @@ LONG = dict(width=10000, max_length=160000, mass_span=160000)
 @pytest.mark.parametrize("kw,code", COMMON + [
     (dict(cache_dtype=F16), UNSUPPORTED), (dict(cache_dtype=F32), UNSUPPORTED), (dict(k_scale=FAKE), INVALID),
     (dict(cache_dtype=E2M1), INVALID), (dict(cache_dtype=E2M1, k_scale=FAKE), INVALID), (dict(mass=None), INVALID),
-    (dict(mass=ODD), INVALID), (dict(mass_span=159), INVALID), (dict(mass_span=1 << 31), INVALID), (LONG, WORKSPACE),
+    (dict(mass_span=159), INVALID), (dict(mass_span=1 << 31), INVALID), (LONG, WORKSPACE),
     (dict(LONG, ws=FAKE, ws_bytes=2 * 8 * 160000 * 4), WORKSPACE),
     # More blocks for the join than a launch has.
     (dict(batch=65535, hq=65535, hk=1), UNSUPPORTED)])

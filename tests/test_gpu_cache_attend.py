@@ -235,6 +235,17 @@ def test_masses_add_up_to_the_heads():
     assert bool(((mass.double().sum(2) - 21).abs() < 21 * 2.0 ** -16).all())
 
 
+def test_masses_without_alignment():
+    """One sequence's part of an array of odd spans."""
+    import paper_2608_13226_amd as cp
+    for lengths in ([37], [3001]):
+        a = _data(lengths, 8, 2, 64, 16, BF)
+        pool = torch.zeros(3, 2, 3003, device="cuda").flatten()[1:]
+        mass = pool[:2 * 3003].view(1, 2, 3003)
+        _check_mass(a, span=3003, start=mass)
+        assert not bool(pool[2 * 3003:].any())
+
+
 def test_long_caches():
     """Slots past 2^31 bytes of codes and a sequence of 200000 tokens."""
     import paper_2608_13226_amd as cp

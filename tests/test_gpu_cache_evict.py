@@ -167,6 +167,15 @@ def test_all_masses_equal_in_a_long_sequence():
     _check(a, 20000, 64, 4)
 
 
+@pytest.mark.parametrize("n,keep", [(3000, 2900), (9000, 5000), (30000, 20000)])
+def test_masses_without_alignment(n, keep):
+    a = _data([n], 2, 64, 16, "bf16")
+    x = a["mass"]
+    a["mass"] = torch.empty(x.numel() + 1, device="cuda")[1:].view(x.shape)
+    a["mass"].copy_(x)
+    _check(a, keep, 10, 2, in_place=True)
+
+
 def test_exponents_without_alignment():
     a = _data([3000, 700], 2, 128, 16, "e2m1")
     for name in ("k_scale", "v_scale"):
