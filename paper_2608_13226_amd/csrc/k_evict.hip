@@ -63,6 +63,20 @@ __device__ __forceinline__ int wave_upto(int x) {
   return x;
 }
 
+// Of one number a wave of the block: the sum of the lower waves', and of all.  A lane takes a
+// wave's: all sixteen in each lane took a third of a selection's time.
+__device__ __forceinline__ int waves_below(const int* part, int wave, int* all = nullptr) {
+  static_assert(kWaves == 16, "a row of lanes has the waves");
+  const int v = part[threadIdx.x % kWaves];
+  int upto = v;
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, false);
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, false);
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, false);
+  upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, false);
+  if (all) *all = __builtin_amdgcn_readlane(upto, kWaves - 1);
+  return __builtin_amdgcn_readlane(upto, wave) - __builtin_amdgcn_readlane(v, wave);
+}
+
 // Counts of a digit with BINS values, COPIES each.
 template <int BINS, int COPIES>
 struct Digits {
@@ -78,7 +92,7 @@ struct Digits {
   // The digit at which the counts from the highest on reach `rest` (1 <= rest <= their
   // sum), and how many are left at it.  The block has synchronised after its last add.
   __device__ __forceinline__ uint32_t find(int& rest) {
-    const int wave = threadIdx.x / kWave, top = BINS - 1 - int(threadIdx.x) * kPer;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave), top = BINS - 1 - int(threadIdx.x) * kPer;
     int c[kPer], sum = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -90,8 +104,7 @@ struct Digits {
     const int here = wave_upto(sum);
     if (threadIdx.x % kWave == kWave - 1) upto[wave] = here;
     lds_sync();
-    int before = here - sum;
-    for (int w = 0; w < wave; ++w) before += upto[w];
+    int before = here - sum + waves_below(upto, wave);
     if (before < rest && rest <= before + sum) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -226,7 +239,7 @@ __global__ __launch_bounds__(kSelect) void evict_one_kernel(KvEvictParams p) {
   __shared__ uint64_t s_above[kWords], s_equal[kWords];
   __shared__ int s_at[kWords], s_part[2][kWaves];
   __shared__ uint32_t s_to[FEW ? kFewRows : 1], s_from[FEW ? kFewRows : 1];     // tokens, then their rows
-  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int kh = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = tokens_of(p, b), keep = int(p.keep), recent = int(p.recent), sink = int(p.sink), m = min(n, keep);
   const int64_t head = int64_t(b) * p.hk + kh;
   const float* mass = p.mass + head * p.span;
@@ -294,8 +307,7 @@ __global__ __launch_bounds__(kSelect) void evict_one_kernel(KvEvictParams p) {
   const int equal_upto = wave_upto(__popcll(equal));
   if (lane == kWave - 1) s_part[0][wave] = equal_upto;
   lds_sync();
-  int left = ties - (equal_upto - __popcll(equal));
-  for (int w = 0; w < wave; ++w) left -= s_part[0][w];
+  const int left = ties - (equal_upto - __popcll(equal)) - waves_below(s_part[0], wave);
   uint64_t over = equal;                                    // ties that leave
   for (int i = 0; i < left && over != 0u; ++i) over &= over - 1;
   uint64_t stays = 0u;
@@ -311,12 +323,8 @@ __global__ __launch_bounds__(kSelect) void evict_one_kernel(KvEvictParams p) {
   const int upto = wave_upto(count);
   if (lane == kWave - 1) s_part[1][wave] = upto;
   lds_sync();
-  int before = upto - count, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    const int v = s_part[1][w];
-    if (w < wave) before += v;
-    total += v;
-  }
+  int total;
+  const int before = upto - count + waves_below(s_part[1], wave, &total);
   total &= 0xffff;
   if (tid < words) {
     s_above[tid] = stays;
@@ -461,7 +469,7 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
   __shared__ Digits<kBuckets, 1> s_top;
   __shared__ int s_part[3][kWaves];
   const Chunk c(p);
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (c.end == 0 || c.want == 0) return;
   int sum = 0;
 #pragma unroll 16
@@ -484,8 +492,7 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
     s_part[2][wave] = high;
   }
   lds_sync();
-  int at = 0;
-  for (int w = 0; w < wave; ++w) at += s_part[0][w];
+  int at = waves_below(s_part[0], wave);
   uint32_t* some = c.ws + c.l.some + c.j0;
   c.each([&](int j, bool here, float m) {
     const uint32_t r = rank_of(m);
@@ -495,13 +502,10 @@ __global__ __launch_bounds__(kSelect) void evict_bucket_kernel(KvEvictParams p) 
     if (yes) some[at + lanes_below(all)] = (r & 0x3fffffu) | uint32_t(j < c.front) << 31;
     at += __popcll(all);
   });
-  if (tid < 4) {
+  if (wave < 4) {
     int x = int(bucket);
-    if (tid < 3) {
-      x = 0;
-      for (int w = 0; w < kWaves; ++w) x += s_part[tid][w];
-    }
-    c.ws[c.l.stats + int64_t(blockIdx.x) * 4 + tid] = uint32_t(x);
+    if (wave < 3) waves_below(s_part[wave], 0, &x);
+    if (lane == 0) c.ws[c.l.stats + int64_t(blockIdx.x) * 4 + wave] = uint32_t(x);
   }
   // (Every block finds the same; the first leaves it.)
   if (blockIdx.x == 0 && tid == 0) c.ws[c.l.ties] = uint32_t(ties);
@@ -513,7 +517,7 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
   __shared__ int s_equal[64], s_low[64], s_high[64], s_equal_low[64];
   __shared__ int s_wave[4][kWaves];
   const Chunk c(p);
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   int32_t* kept = p.kept + c.head * p.keep;
   float* fresh = reinterpret_cast<float*>(c.ws + c.l.mass);
   if (c.end == 0) {
@@ -626,12 +630,15 @@ __global__ __launch_bounds__(kSelect) void evict_border_kernel(KvEvictParams p) 
     s_wave[3][wave] = more_high;
   }
   lds_sync();
-  for (int w = 0; w < wave; ++w) {
-    const int a = min(c.j1, c.j0 + w * c.per), z = max(a, min(c.front, min(c.j1, a + c.per)));
-    const int taken = min(max(ties - tie0, 0), s_wave[0][w]), taken_low = min(taken, s_wave[1][w]);
-    tie0 += s_wave[0][w];
-    gap0 += z - a - s_wave[2][w] - taken_low;
-    go0 += s_wave[3][w] + taken - taken_low;
+  {
+    // Lane w has wave w.
+    const int w = lane % kWaves, a = min(c.j1, c.j0 + w * c.per), z = max(a, min(c.front, min(c.j1, a + c.per)));
+    const int n = lane < kWaves ? s_wave[0][w] : 0, seen = tie0 + wave_upto(n) - n;
+    const int taken = min(max(ties - seen, 0), n), taken_low = min(taken, s_wave[1][w]);
+    const int gap = lane < kWaves ? z - a - s_wave[2][w] - taken_low : 0, go = lane < kWaves ? s_wave[3][w] + taken - taken_low : 0;
+    tie0 = __builtin_amdgcn_readlane(seen, wave);
+    gap0 += __builtin_amdgcn_readlane(wave_upto(gap) - gap, wave);
+    go0 += __builtin_amdgcn_readlane(wave_upto(go) - go, wave);
   }
   int *vacant = reinterpret_cast<int*>(c.ws + c.l.vacant), *movers = reinterpret_cast<int*>(c.ws + c.l.movers);
   float* mover_mass = reinterpret_cast<float*>(c.ws + c.l.mover_mass);
