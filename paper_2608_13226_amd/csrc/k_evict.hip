@@ -25,9 +25,9 @@
 //   evict_shift  the last rows, once the places at the front are empty
 //
 // Bound by the launches and barriers between dependent steps: 8 sequences of up to 1702
-// tokens of 4 heads, 64 of each out, 12.5 us; 131072 tokens of 4 heads halved 75 us
+// tokens of 4 heads, 64 of each out, 11.4 us; 131072 tokens of 4 heads halved 56 us
 // without the gaps between five launches, of which the rows, in scattered pieces of 64
-// and 4 bytes, take 20.
+// and 4 bytes, take 17 to 24.
 #include <algorithm>
 
 #include "launch.h"
@@ -218,13 +218,13 @@ __host__ __device__ inline Lists lists_of(int64_t keep, int64_t recent, int64_t 
 // ---------------------------------------------------------------------------
 // Up to 16384 tokens: selected by one block.
 
-// A sequence's tokens are in one block's LDS up to here: 7.3 us for 64 tokens, 0.8 for each 1024
-// more.  In chunks over the chip it is the launches' time (40 heads of 16384 tokens, 1639 kept: 32.2
-// us with three launches and 35.4 with five; a sequence of 16384 of 4 heads 26.4 and 28.5).
+// A sequence's tokens are in one block's LDS up to here: 6.2 us for 64 tokens, 0.8 for each 1024
+// more.  In chunks over the chip it is the launches' time (40 heads of 16384 tokens, 1639 kept: 30.4
+// us with three launches and 35.4 with five; a sequence of 16384 of 4 heads 24.5 and 28.5).
 constexpr int kOneTokens = 16384, kWords = kOneTokens / kWave;
 // As many moves are made by the same block, which has one compute unit's share of the memory's rate:
-// vacant places and `recent` (32 heads of 4096 tokens, 1000 kept: 24.7 us; with two more launches
-// and 2000 kept 28.2, where one took 34.7).
+// vacant places and `recent` (32 heads of 4096 tokens, 1000 kept: 23.5 us; with two more launches
+// and 2000 kept 26.8, where one took 34.7).
 constexpr int kFewRows = 1024;
 using Top = Digits<4096, 2>;        // of the rank's highest 12 bits: most masses share an octave or two, and
 using Low = Digits<1024, 1>;        // additions to one address wait for each other; then two digits of 10
