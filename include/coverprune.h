@@ -631,7 +631,7 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
  *   code  of x / s, at most 6 in size, rounded to nearest, ties to the even code:
  *         0, 1/2, 1, 3/2, 2, 3, 4, 6 are codes 0 to 7, with a sign 8 to 15
  * Keys are rotated in float64 for it, so that codes are those of the formula, up
- * to float64's own rounding.  An infinity or NaN among the 32 makes them all
+ * to float64's own rounding (magnitude is a double, within float32's range).  An infinity or NaN among the 32 makes them all
  * NaN: the byte is 255 (and the codes 0).
  *
  *   q, k, v, dtype, positions, slots, inv_freq, rot, interleaved, magnitude, q_out
@@ -645,7 +645,7 @@ cp_status coverprune_paged_attention(const void* q, cp_dtype dtype, int64_t batc
 cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
                                 const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
-                                int32_t interleaved, float magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
+                                int32_t interleaved, double magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
                                 int64_t pages, int64_t page_size, uint8_t* k_scale, uint8_t* v_scale, void* stream);
 
 /* Keys and values of some slots of a paged cache as dense rows.
@@ -721,7 +721,8 @@ cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t
  *   kept       [batch, hk, keep] int32 output: which token is now at each place, -1
  *              from the new length on
  *   mass_out   [batch, hk, mass_span] float output, may be mass: the masses in the new
- *              order, 0 from the new length on (otherwise without overlap)
+ *              order (-0 may become 0, a NaN another), 0 from the new length on;
+ *              otherwise without overlap
  *   lengths_out  [batch] int32 output that does not overlap lengths: the new lengths, at
  *              most keep
  *   workspace  coverprune_kv_evict_workspace bytes

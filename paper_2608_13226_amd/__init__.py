@@ -191,8 +191,8 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.coverprune_paged_attention.argtypes = [vp, dt, i64, i64, i64, i64, vp, vp, dt, i64, i64, vp, vp, vp, i64, vp, i64,
                                                i64, f32, vp, vp, vp, sz, vp]
     lib.coverprune_paged_attention.restype = st
-    lib.coverprune_kv_append4.argtypes = [vp, i64, vp, i64, vp, i64, dt, i64, i64, i64, i64, vp, vp, vp, i64, i32, f32, vp,
-                                          vp, vp, i64, i64, vp, vp, vp]
+    lib.coverprune_kv_append4.argtypes = [vp, i64, vp, i64, vp, i64, dt, i64, i64, i64, i64, vp, vp, vp, i64, i32, ctypes.c_double,
+                                          vp, vp, vp, i64, i64, vp, vp, vp]
     lib.coverprune_kv_append4.restype = st
     lib.coverprune_kv_gather.argtypes = [vp, vp, dt, i64, i64, i64, i64, vp, vp, vp, i64, vp, vp, dt, vp]
     lib.coverprune_kv_gather.restype = st

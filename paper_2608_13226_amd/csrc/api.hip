@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -912,7 +913,7 @@ static bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
 cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, cp_dtype dtype, int64_t tokens, int64_t hq, int64_t hk, int64_t d,
                                 const int32_t* positions, const int64_t* slots, const float* inv_freq, int64_t rot,
-                                int32_t interleaved, float magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
+                                int32_t interleaved, double magnitude, void* q_out, uint8_t* k_cache, uint8_t* v_cache,
                                 int64_t pages, int64_t page_size, uint8_t* k_scale, uint8_t* v_scale, void* stream) {
   if (tokens < 0 || tokens >= (int64_t(1) << 31))
     return fail(CP_ERR_INVALID_ARG, "tokens = %lld outside [0, 2^31)", (long long)tokens);
@@ -923,7 +924,7 @@ cp_status coverprune_kv_append4(const void* q, int64_t q_stride, const void* k, 
   if (page_size < 1 || page_size > (1 << 20)) return fail(CP_ERR_INVALID_ARG, "page_size = %lld outside [1, 2^20]", (long long)page_size);
   if (pages < 1 || pages > (int64_t(1) << 40)) return fail(CP_ERR_INVALID_ARG, "pages = %lld outside [1, 2^40]", (long long)pages);
   if (!half_type(dtype)) return fail(CP_ERR_UNSUPPORTED, "dtype %d: bf16 or f16", (int)dtype);
-  if (!std::isfinite(magnitude)) return fail(CP_ERR_INVALID_ARG, "magnitude must be finite");
+  if (!(std::fabs(magnitude) <= FLT_MAX)) return fail(CP_ERR_INVALID_ARG, "magnitude must be finite in float32");
   if ((q && q_stride < hq * d) || k_stride < hk * d || v_stride < hk * d)
     return fail(CP_ERR_INVALID_ARG, "a token stride is smaller than a token's heads");
   if (tokens == 0) return ok();

@@ -414,7 +414,7 @@ PyObject* kv_append4(PyObject* const* a) {
     raise(PyExc_ValueError, "the caches are for %lld heads of %lld, k has %lld of %lld", (long long)c.hk, (long long)c.d, (long long)hk, (long long)d);
   const Tensor qo = q.defined() ? output(a[12], "q_out", t, {tokens, hq, d}, dev) : Tensor();
   check(coverprune_kv_append4(at_of<void>(q), qstride, k.data_ptr(), kstride, v.data_ptr(), vstride, code(t), tokens, hq, hk, d,
-                              at_of<int32_t>(pos), at_of<int64_t>(slots), at_of<float>(inv), 2 * half, inter, float(magnitude),
+                              at_of<int32_t>(pos), at_of<int64_t>(slots), at_of<float>(inv), 2 * half, inter, magnitude,
                               at_of<void>(qo), at_of<uint8_t>(kc), at_of<uint8_t>(vc), c.c.pages, c.c.page, at_of<uint8_t>(ks),
                               at_of<uint8_t>(vs), stream_of(dev)));
   written(qo), written(kc), written(vc), written(ks), written(vs);

@@ -295,7 +295,7 @@ struct KvAppend4Params {
   int64_t tokens, pages;
   int hq, hk, d, rot, page;       // d % 32 == 0
   Divide by_page, by_runs;        // by d / 8
-  float magnitude;
+  double magnitude;
   bool interleaved;
   ServeType type;
 };

@@ -41,7 +41,7 @@ def _append(lib, **kw):
     (dict(tokens=-1), INVALID), (dict(tokens=1 << 31), INVALID), (dict(hq=0), INVALID), (dict(hk=0), INVALID), (dict(d=0), UNSUPPORTED),
     (dict(d=48), UNSUPPORTED), (dict(d=4128), UNSUPPORTED), (dict(rot=3), INVALID), (dict(rot=-2), INVALID), (dict(rot=130), INVALID),
     (dict(page_size=0), INVALID), (dict(page_size=(1 << 20) + 1), INVALID), (dict(pages=0), INVALID), (dict(dtype=F32), UNSUPPORTED),
-    (dict(dtype=E2M1), UNSUPPORTED), (dict(magnitude=math.nan), INVALID), (dict(q_stride=1000), INVALID), (dict(k_stride=255), INVALID),
+    (dict(dtype=E2M1), UNSUPPORTED), (dict(magnitude=math.nan), INVALID), (dict(magnitude=-1e39), INVALID), (dict(q_stride=1000), INVALID), (dict(k_stride=255), INVALID),
     (dict(v_stride=0), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(positions=None), INVALID),
     (dict(slots=None), INVALID), (dict(inv_freq=None), INVALID), (dict(q_out=None), INVALID), (dict(k_cache=None), INVALID),
     (dict(v_cache=None), INVALID), (dict(k_scale=None), INVALID), (dict(v_scale=None), INVALID), (dict(k_cache=ODD), INVALID),

@@ -149,6 +149,22 @@ def test_keys_past_float32_saturate():
     assert bool((_rows(caches[2], slots.cpu()) == 252).all())
 
 
+@pytest.mark.parametrize("t", [BF, F16])
+@pytest.mark.parametrize("inter", [False, True])
+def test_magnitude_is_taken_in_64_bits(t, inter):
+    """1.2 * 5 is 6 in float64, where a block keeps its power; with 1.2 rounded to float32, 4e-8 too large, it would be past it."""
+    import paper_2608_13226_amd as cp
+    assert 1.2 * 5 == 6.0 and 1.2 * 1.25 == 1.5 and 5 * float(torch.tensor(1.2)) > 6.0
+    q, k, v, pos, slots, inv, caches = _data(3, 1, 1, 32, 32, 16, t)
+    k = torch.full_like(k, 1.25)
+    k[:, :, 0] = 5.0
+    pos.zero_()
+    cp.kv_append4(None, k, v, pos, slots, inv, *caches, interleaved=inter, magnitude=1.2)
+    assert bool((_rows(caches[2], slots.cpu()) == 127).all())
+    codes = cache_ref.unpack(_rows(caches[0], slots.cpu()))
+    assert bool((codes[..., 0] == 7).all()) and bool((codes[..., 1:] == 3).all())
+
+
 def test_no_tokens():
     import paper_2608_13226_amd as cp
     q, k, v, pos, slots, inv, caches = _data(0, 2, 1, 64, 64, 16, BF)
