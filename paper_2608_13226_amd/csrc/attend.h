@@ -24,8 +24,10 @@
 //
 // Caches of 4 bits are e2m1 codes with a power of two for each 32 dims: an
 // instruction widens two codes and applies the power, exactly.  16 sequences of
-// 65536 tokens of 4 heads of 128 in 107 us (5.1 TB/s); with heads of 64 the vector
-// instructions bound it (24 ragged ones of 16 such heads 28 us, 3.1 TB/s).
+// 65536 tokens of 4 heads of 128 in 107 us (5.1 TB/s); 24 of 28000 of 16 heads of 64 in
+// 170 us (4.3 TB/s).  On shorter ones, 24 of up to 6900 in 29 us (3.1 TB/s) and 5 for the join, start
+// and end weigh more; two tiles that share the columns of one softmax where query heads
+// are few (a tenth fewer vector instructions) changed nothing.
 //
 // MASS: the kernel also leaves its scores, and what each token's weights come to
 // is added to its mass once the sums of all runs are known: by the same block
