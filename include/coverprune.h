@@ -713,8 +713,8 @@ cp_status coverprune_paged_attention_mass(const void* q, cp_dtype dtype, int64_t
  *              CP_E2M1; d a multiple of 8 (CP_E2M1: of 32), at most 4096;
  *              pages * hk * page_size < 2^32
  *   k_scale, v_scale  CP_E2M1: the exponents, which move with their rows; otherwise NULL
- *   table, lengths, max_length  as for coverprune_paged_attention.  Pages that two
- *              sequences share are the caller's error.
+ *   table, lengths, max_length  as for coverprune_paged_attention, but max_length <= 2^30;
+ *              batch * hk <= 2^24.  Pages that two sequences share are the caller's error.
  *   mass       [batch, hk, mass_span] float, mass_span >= max_length (mass, mass_out, kept and
  *              lengths_out aligned as their elements are)
  *   keep       1 <= keep < 2^31; recent >= 0, sink >= 0, recent + sink <= keep

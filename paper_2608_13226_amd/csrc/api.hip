@@ -1019,8 +1019,11 @@ static cp_status check_evict(int64_t batch, int64_t hk, int64_t keep, int64_t re
   if (recent < 0 || sink < 0 || recent > keep || sink > keep - recent)
     return fail(CP_ERR_INVALID_ARG, "recent = %lld and sink = %lld must be >= 0, together at most keep = %lld", (long long)recent,
                 (long long)sink, (long long)keep);
-  if (max_length < 1 || max_length >= (int64_t(1) << 31) - 2048)
-    return fail(CP_ERR_INVALID_ARG, "max_length = %lld outside [1, 2^31 - 2048)", (long long)max_length);
+  // Tokens are counted in 32 bits, with a chunk or a grid's step on top.
+  if (max_length < 1 || max_length > (int64_t(1) << 30))
+    return fail(CP_ERR_INVALID_ARG, "max_length = %lld outside [1, 2^30]", (long long)max_length);
+  if (batch * hk > (1 << 24))
+    return fail(CP_ERR_UNSUPPORTED, "batch = %lld sequences of %lld heads are too many for one call", (long long)batch, (long long)hk);
   return CP_OK;
 }
 

@@ -133,6 +133,7 @@ BIG = dict(width=10000, max_length=160000, mass_span=160000, keep=80000)
     (dict(keep=-1), INVALID), (dict(keep=1 << 31), INVALID), (dict(recent=-1), INVALID), (dict(recent=101), INVALID),
     (dict(sink=-1), INVALID), (dict(sink=91), INVALID), (dict(recent=2 ** 62, sink=2 ** 62), INVALID), (dict(max_length=0), INVALID),
     (dict(max_length=161), INVALID), (dict(max_length=(1 << 31) - 2048, width=1 << 27), INVALID), (dict(mass_span=159), INVALID),
+    (dict(max_length=(1 << 30) + 1, width=1 << 27, mass_span=(1 << 30) + 1), INVALID), (dict(batch=65535, hk=257), UNSUPPORTED),
     (dict(mass_span=1 << 31), INVALID), (dict(page_size=0), INVALID), (dict(pages=0), UNSUPPORTED), (dict(pages=1 << 28), UNSUPPORTED),
     (dict(width=0), INVALID), (dict(cache_dtype=F32), UNSUPPORTED), (dict(cache_dtype=9), UNSUPPORTED), (dict(d=0), UNSUPPORTED),
     (dict(d=4), UNSUPPORTED), (dict(d=100), UNSUPPORTED), (dict(d=4104), UNSUPPORTED), (dict(cache_dtype=E2M1, d=40), UNSUPPORTED),
@@ -160,7 +161,8 @@ def test_workspaces(lib):
     # The scores beside what the other call takes.
     for case in ((1, 28, 4, 128, 131072, 0), (16, 28, 4, 128, 65536, 0), (3, 40, 2, 64, 500, 0), (2, 20, 1, 256, 600, 100)):
         assert mass(*case) >= size(*case) + 4 * case[0] * case[1] * min(case[4], case[5] or case[4])
-    for bad in ((-1, 2, 10, 1, 100), (1, 0, 10, 1, 100), (1, 2, 0, 0, 100), (1, 2, 10, 11, 100), (1, 2, 10, -1, 100), (1, 2, 10, 1, 0)):
+    for bad in ((-1, 2, 10, 1, 100), (1, 0, 10, 1, 100), (1, 2, 0, 0, 100), (1, 2, 10, 11, 100), (1, 2, 10, -1, 100), (1, 2, 10, 1, 0),
+                (1, 2, 10, 1, (1 << 30) + 1), (65535, 65535, 1 << 29, 0, 1 << 30)):
         assert evict(*bad) == 0
     assert evict(4, 2, 100, 10, 90) == 0
     assert evict(1, 1, 50000, 100, 100000) >= 4 * (2 * 49900 + 50000)
