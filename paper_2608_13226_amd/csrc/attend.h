@@ -232,19 +232,14 @@ struct RawKey<T, Held::kE2m1, D> {
 // part of 0: bfloat16's parts are cut below what they are parts of, so that
 // there is always a rest (p from 2^-90 on), and a float16 p's rest meets the
 // values through finite2.
-// Values of 4 bits are finite, and what out's rounding to 2^-9 leaves of p is well
-// within two parts' 2^-18 (16 x 65536 tokens 109.6 us, with three parts 113.7).
-template <class T, Held C> constexpr int kParts = std::is_same_v<T, Bf16> && C != Held::kE2m1 ? 3 : 2;
-template <class T, int PARTS>
+// (Over 4 bits two parts of bfloat16, 2^-17 of p, took 4 % less, 111 against 115 us for
+// 16 x 65536 tokens, and put two to ten times as many results a step of bfloat16 off.)
+template <class T> constexpr int kParts = 3;
+template <> constexpr int kParts<F16> = 2;
+template <class T>
 __device__ __forceinline__ void split(float a, float b, uint32_t* part);
 template <>
-__device__ __forceinline__ void split<Bf16, 2>(float a, float b, uint32_t* part) {
-  part[0] = pack2<Bf16>(a, b);
-  const float2 r = unpack2<Bf16>(part[0]);
-  part[1] = pack2<Bf16>(a - r.x, b - r.y);
-}
-template <>
-__device__ __forceinline__ void split<Bf16, 3>(float a, float b, uint32_t* part) {
+__device__ __forceinline__ void split<Bf16>(float a, float b, uint32_t* part) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     // The float below, or 0.
@@ -256,7 +251,7 @@ __device__ __forceinline__ void split<Bf16, 3>(float a, float b, uint32_t* part)
   part[2] = pack2<Bf16>(a, b);
 }
 template <>
-__device__ __forceinline__ void split<F16, 2>(float a, float b, uint32_t* part) {
+__device__ __forceinline__ void split<F16>(float a, float b, uint32_t* part) {
   part[0] = pack2<F16>(a, b);
   const float2 r = unpack2<F16>(part[0]);
   part[1] = pack2<F16>(a - r.x, b - r.y);
@@ -407,14 +402,14 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 1 : 2) void attend_kernel(AttendP
     }
     // While no score is above -inf, each p is 0.
     const float base = m == -INFINITY ? 0.f : m;
-    constexpr int kOf = kParts<T, C>;
+    constexpr int kOf = kParts<T>;
     u32x4 part[kOf];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float a = __builtin_amdgcn_exp2f(x[i] - base), e = __builtin_amdgcn_exp2f(x[i + 1] - base);
       l += a + e;
       uint32_t w[kOf];
-      split<T, kOf>(a, e, w);
+      split<T>(a, e, w);
 #pragma unroll
       for (int n = 0; n < kOf; ++n) part[n][i / 2] = w[n];
     }

@@ -1,0 +1,60 @@
+"""How many bits of a weight reach the values that are attended to, and of a rotated key the codes it is held in."""
+import math
+
+import pytest
+
+from tests import cache_ref, serving_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF, F16, E4M3 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+def _attend(a, mass, **kw):
+    import paper_2608_13226_amd as cp
+    scales = dict(k_scale=a["k_scale"], v_scale=a["v_scale"])
+    args = a["q"], a["k_cache"], a["v_cache"]
+    if mass:
+        hk, span = a["k_cache"].shape[1], a["table"].shape[1] * a["k_cache"].shape[2]
+        m = torch.zeros(a["q"].shape[0], hk, span, device="cuda")
+        return cp.paged_attention_mass(*args, a["table"], a["lengths"], m, **scales, **kw)
+    if a["k_cache"].dtype == torch.uint8:
+        return cp.paged_attention4(*args, a["k_scale"], a["v_scale"], a["table"], a["lengths"], **kw)
+    return cp.paged_attention(*args, a["table"], a["lengths"], **scales, **kw)
+
+
+@pytest.mark.parametrize("mass", [False, True])
+@pytest.mark.parametrize("held", ["same", "e4m3", "e2m1"])
+@pytest.mark.parametrize("t", [BF, F16])
+def test_weights_keep_float32s_bits(t, held, mass):
+    """Two tokens whose values cancel and whose weights differ by 2^-14: what is left shows each weight's last bits.  (A third,
+    without a value, has the largest weight, a power of two.)
+
+    Relative to a weight: its exponent x, below 2.9, is rounded twice, and once more with 8 to 16 taken off it,
+    ln 2 (2 * 2.9 * 2^-24 + 2^-21) = 1.2 * 2^-21; the exponential to a step, 2^-23; float16's two parts leave 2^-22, bfloat16's
+    three 2^-25; six additions and two products of at most 1 add 8 * 2^-24 / 2.  Together below 2.5 * 2^-21."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    batch, heads, d, page = 64, 16, 64, 16
+    k, v = (torch.zeros(1, 1, page, d, device="cuda") for _ in range(2))
+    k[0, 0, :3, 0] = torch.tensor([1.0, 1.0, 1.5])
+    k[0, 0, 1, 32] = 2.0 ** -6
+    v[0, 0, 0], v[0, 0, 1] = 1.0, -1.0
+    caches, scales = [], []
+    for x in (k, v):
+        codes, e = cache_ref.cut_cache(x, t) if held == "e2m1" else (x.to(E4M3 if held == "e4m3" else t), None)
+        caches.append(codes)
+        scales.append(e)
+        if held == "e2m1":
+            assert torch.equal(cache_ref.values(codes, e), ref.d64(x))
+    q = torch.zeros(batch, heads, d, device="cuda")
+    q[:, :, 0] = 0.5 + 1.5 * torch.rand(batch, heads, device="cuda", generator=g)
+    q[:, :, 32] = 2.0 ** -8 * (1 + torch.rand(batch, heads, device="cuda", generator=g))
+    q = q.to(t)
+    a = dict(q=q, k_cache=caches[0], v_cache=caches[1], table=torch.zeros(batch, 1, dtype=torch.int32, device="cuda"),
+             lengths=torch.full((batch,), 3, dtype=torch.int32, device="cuda"), k_scale=scales[0], v_scale=scales[1])
+    out = _attend(a, mass, max_length=3, scale=1.0)
+    x, more = ref.d64(q)[:, :, 0], ref.d64(q)[:, :, 32] * 2.0 ** -6
+    p = [torch.exp(-x / 2), torch.exp(more - x / 2), torch.ones_like(x)]
+    want, size = (y[..., None].expand(batch, heads, d) / sum(p)[..., None] for y in (p[0] - p[1], p[0] + p[1]))
+    ref.assert_close(out, want, t, 2.5 * 2.0 ** -21 * size, "out")
