@@ -667,7 +667,7 @@ cp_status coverprune_kv_gather(const void* k_cache, const void* v_cache, cp_dtyp
  *
  *   k_cache, v_cache, k_scale, v_scale  as coverprune_kv_append4 writes them; what they
  *              stand for is taken to dtype (exactly, where dtype has been theirs from the
- *              start).  Values that are NaN count where their token's weight is 0, too.
+ *              start; what it does not hold is infinite).  Values that are NaN count where their token's weight is 0, too.
  *   the rest   as for coverprune_paged_attention, the workspace too
  */
 cp_status coverprune_paged_attention4(const void* q, cp_dtype dtype, int64_t batch, int64_t hq, int64_t hk, int64_t d,

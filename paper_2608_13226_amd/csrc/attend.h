@@ -144,6 +144,12 @@ struct RawValue<T, Held::kE2m1, D> {
     const int byte = q < 4 * L::n8 ? q % 4 : q < 4 * L::n8 + 2 * L::n4 ? q - 4 * L::n8 : 0;
     return open2<T>(w[run], power_of(e[run]), byte);
   }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t most = e[0];
+#pragma unroll
+    for (int i = 1; i < kRuns; ++i) most = max(most, e[i]);
+    return most;
+  }
   // Codes and exponent both, so that a block without a value (exponent 255) counts nothing.
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -413,6 +419,15 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 1 : 2) void attend_kernel(AttendP
 #pragma unroll
       for (int n = 0; n < kOf; ++n) part[n][i / 2] = w[n];
     }
+    // Whether values may be infinite in float16.  6 times 2^13 is not, and 4-bit blocks past that are rare,
+    // so they are looked for (24 sequences of up to 6900 tokens 33.8 us; 38.5 with finite2 for all, 32.5 with neither).
+    bool past = std::is_same_v<T, F16> && C == Held::kSame;
+    if constexpr (std::is_same_v<T, F16> && C == Held::kE2m1) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = max(most, val[j].largest());
+      past = __any(most > 127 + 13);
+    }
 #pragma unroll
     for (int i = 0; i < L::pairs; ++i) {
       u32x4 even, odd;
@@ -424,7 +439,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 1 : 2) void attend_kernel(AttendP
       }
 #pragma unroll
       for (int n = 0; n < kOf; ++n) {
-        if (std::is_same_v<T, F16> && C == Held::kSame && n == 1) {
+        if (std::is_same_v<T, F16> && C != Held::kE4m3 && n == 1 && past) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             even[j] = finite2(even[j]);

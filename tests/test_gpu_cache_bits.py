@@ -58,3 +58,34 @@ def test_weights_keep_float32s_bits(t, held, mass):
     p = [torch.exp(-x / 2), torch.exp(more - x / 2), torch.ones_like(x)]
     want, size = (y[..., None].expand(batch, heads, d) / sum(p)[..., None] for y in (p[0] - p[1], p[0] + p[1]))
     ref.assert_close(out, want, t, 2.5 * 2.0 ** -21 * size, "out")
+
+
+@pytest.mark.parametrize("mass", [False, True])
+@pytest.mark.parametrize("t,byte", [(F16, 141), (F16, 150), (F16, 254), (BF, 253), (BF, 254)])
+@pytest.mark.parametrize("lengths,d,page", [([1, 40, 300], 128, 16), ([700, 65], 64, 64), ([3000], 96, 32)])
+def test_values_past_the_queries_type_are_infinite(lengths, d, page, t, byte, mass):
+    """A cache made from another type, or by another program: what the type does not hold is an infinity, which makes its
+    dimension infinite (two of both signs: NaN) and no other."""
+    g = torch.Generator(device="cuda").manual_seed(d + byte)
+    batch, hq, hk = len(lengths), 4, 2
+    width = (max(lengths) + page - 1) // page
+    table = torch.randperm(batch * width, device="cuda", generator=g).view(batch, width).to(torch.int32)
+    caches, scales = [], []
+    for _ in range(2):
+        codes, e = cache_ref.cut_cache(torch.randn(batch * width, hk, page, d, device="cuda", generator=g), t)
+        caches.append(codes)
+        scales.append(e)
+    # The first and the last token's second block of each sequence.
+    for b, n in enumerate(lengths):
+        for j in (0, n - 1):
+            scales[1][int(table[b, j // page]), :, j % page, 1] = byte
+    q = torch.randn(batch, hq, d, device="cuda", generator=g).to(t)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    a = dict(q=q, k_cache=caches[0], v_cache=caches[1], table=table, lengths=n, k_scale=scales[0], v_scale=scales[1])
+    out = _attend(a, mass, max_length=max(lengths))
+    held = [cache_ref.values(c, e).to(t).cuda() for c, e in zip(caches, scales)]
+    want, _, size = ref.attend(q, *held, table, n)
+    assert bool(torch.isinf(want).any()) and bool(torch.isfinite(want[..., :32]).all())
+    # As in the attention's own tests.
+    size = torch.where(torch.isfinite(size), size, torch.zeros_like(size))
+    ref.assert_close(out, want, t, 2.0 ** -24 * (60 * (d / 32 + 8) + max(lengths) / 32 + 100) * size, "out")
