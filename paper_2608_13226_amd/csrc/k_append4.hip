@@ -23,12 +23,12 @@
 namespace cp {
 namespace {
 
-// float64 to float32, rounded to odd: of the 29 bits that go, whether any was set stays in the
-// last one of the others, and the conversion is exact.  (Past float32's range: infinite.)
+// float64 to float32, rounded to odd at 21 bits after the leading one: of the 31 that go, whether any
+// was set stays in the last one of the others, and the conversion is exact down to 2^-128, below all borders (the
+// lowest is 2^-127, where float32 has 22 such bits).  (Past float32's range: infinite.)
 __device__ __forceinline__ float round_odd(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const uint32_t low = uint32_t(b), kept = (low & 0xe0000000u) | (low & 0x1fffffffu ? 0x20000000u : 0u);
-  return float(__builtin_bit_cast(double, (b & 0xffffffff00000000u) | kept));
+  return float(__builtin_bit_cast(double, (b & 0xffffffff00000000u) | (uint32_t(b) ? 0x80000000u : 0u)));
 }
 
 // Eight elements from element i on, as they are stored.

@@ -89,3 +89,22 @@ def test_values_past_the_queries_type_are_infinite(lengths, d, page, t, byte, ma
     # As in the attention's own tests.
     size = torch.where(torch.isfinite(size), size, torch.zeros_like(size))
     ref.assert_close(out, want, t, 2.0 ** -24 * (60 * (d / 32 + 8) + max(lengths) / 32 + 100) * size, "out")
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("magnitude", [0.5, 0.5 * (1 + 2.0 ** -30), 0.5 * (1 - 2.0 ** -30), 0.5 * (1 + 2.0 ** -23), 0.5 * (1 + 2.0 ** -22)])
+def test_a_key_next_to_the_lowest_border(magnitude, inter):
+    """A quarter of the smallest power, 2^-127, is where code 0 ends, and below float32's normal numbers: a key just
+    above it has code 1 (exact in float64: turned by nothing, times the magnitude)."""
+    import paper_2608_13226_amd as cp
+    k = torch.full((3, 2, 32), 2.0 ** -126, device="cuda").to(BF)
+    k[1], k[2, 0, ::2] = -k[1], 0.0
+    caches = [torch.zeros(3, 2, 1, w, dtype=torch.uint8, device="cuda") for w in (16, 16, 1, 1)]
+    cp.kv_append4(None, k, k, torch.zeros(3, dtype=torch.int32, device="cuda"), torch.arange(3, device="cuda"),
+                  torch.ones(16, device="cuda"), *caches, interleaved=inter, magnitude=magnitude)
+    code, e = cache_ref.blocks(ref.d64(k) * magnitude, BF)
+    assert torch.equal(caches[2][:, :, 0].cpu().int(), e) and bool((e == 2).all())
+    got = cache_ref.unpack(caches[0][:, :, 0])
+    # (-0 where nothing is left of a negative one, and a turned 0 may have either sign.)
+    assert torch.equal(got & 7, code & 7) and torch.equal(got[code & 7 != 0], code[code & 7 != 0])
+    assert bool((code & 7 != 0).any()) == (magnitude > 0.5)
