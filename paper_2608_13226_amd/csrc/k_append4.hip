@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void kv_append4_kernel(KvAppend4Params p, int 
         // What is finite but past float32's range counts as its largest number.
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (fabs(y[j]) < __builtin_inf()) x[j] = float(fmin(fmax(y[j], -3.4028234663852886e38), 3.4028234663852886e38));
+          if (fabs(y[j]) < __builtin_inf()) x[j] = round_odd(fmin(fmax(y[j], -3.4028234663852886e38), 3.4028234663852886e38));
       }
     }
     put(w, x, p.k_cache, p.k_scale);

@@ -108,3 +108,20 @@ def test_a_key_next_to_the_lowest_border(magnitude, inter):
     # (-0 where nothing is left of a negative one, and a turned 0 may have either sign.)
     assert torch.equal(got & 7, code & 7) and torch.equal(got[code & 7 != 0], code[code & 7 != 0])
     assert bool((code & 7 != 0).any()) == (magnitude > 0.5)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("magnitude", [1.0, 1 + 2.0 ** -30, 1 - 2.0 ** -30])
+def test_keys_at_borders_beside_the_largest(magnitude, inter):
+    """Next to an element at the end of float32's range, whose block has the largest power, 2^125, elements just past a border
+    of that power have the code beyond it."""
+    import paper_2608_13226_amd as cp
+    k = torch.full((2, 1, 32), 2.0 ** 123, device="cuda").to(BF)
+    k[:, :, 1::4], k[:, :, 2::4] = 1.25 * 2.0 ** 125, -2.5 * 2.0 ** 125
+    k[:, :, 4::8], k[:, :, 3::8] = 0.75 * 2.0 ** 125, torch.finfo(BF).max
+    caches = [torch.zeros(2, 1, 1, w, dtype=torch.uint8, device="cuda") for w in (16, 16, 1, 1)]
+    cp.kv_append4(None, k, k, torch.zeros(2, dtype=torch.int32, device="cuda"), torch.arange(2, device="cuda"),
+                  torch.ones(16, device="cuda"), *caches, interleaved=inter, magnitude=magnitude)
+    code, e = cache_ref.blocks(ref.d64(k) * magnitude, BF)
+    assert torch.equal(caches[2][:, :, 0].cpu().int(), e) and bool((e == 252).all())
+    assert torch.equal(cache_ref.unpack(caches[0][:, :, 0]), code)
