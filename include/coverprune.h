@@ -688,8 +688,8 @@ cp_status coverprune_paged_attention4(const void* q, cp_dtype dtype, int64_t bat
  *              coverprune_kv_gather
  *   mass       [batch, hk, mass_span] float, mass_span >= max_length; aligned as a float
  *              is, so that sequences of any span can be part of a larger array
- *   workspace  coverprune_paged_attention_mass_workspace bytes, 4 * batch * hq *
- *              max_length of them for the scores
+ *   workspace  coverprune_paged_attention_mass_workspace bytes, enough for every
+ *              cache_dtype, 4 * batch * hq * max_length of them for the scores
  */
 size_t coverprune_paged_attention_mass_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                                  int64_t window);

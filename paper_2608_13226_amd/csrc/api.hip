@@ -771,16 +771,21 @@ static cp_status check_attend(int64_t batch, int64_t hq, int64_t hk, int64_t d, 
   return CP_OK;
 }
 
+// Enough for a cache of any type: those of 4 bits are cut otherwise.
+static size_t attend_query(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length, int64_t window, bool mass) {
+  if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
+  return std::max(cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, mass, false),
+                  cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, mass, true));
+}
+
 size_t coverprune_paged_attention_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                             int64_t window) {
-  if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
-  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, false, false);
+  return attend_query(batch, hq, hk, d, max_length, window, false);
 }
 
 size_t coverprune_paged_attention_mass_workspace(int64_t batch, int64_t hq, int64_t hk, int64_t d, int64_t max_length,
                                                  int64_t window) {
-  if (check_attend(batch, hq, hk, d, max_length, window) != CP_OK || batch == 0) return 0;
-  return cp::attend_workspace_bytes(batch, hq, hk, d, max_length, window, true, false);
+  return attend_query(batch, hq, hk, d, max_length, window, true);
 }
 
 // Pages, table and lengths of a call over a paged cache.
