@@ -695,9 +695,11 @@ struct Plan {
 Plan plan(int64_t batch, int64_t hq, int64_t hk, int64_t span, bool four) {
   const int64_t tiles = (span + kTile - 1) / kTile;
   const int64_t blocks = batch * hk * ((hq / hk + 15) / 16);
-  // 4 bits, up to 128 dims: sixteen waves have 24 tiles sooner than two launches (629 tokens 8.1 us
-  // against 9.3, 760 8.7; but 1000 9.9 against 9.3).
-  if (four && tiles > 16 && tiles <= 24) return {int(tiles), 1, 16};
+  // 4 bits, up to 128 dims, fewer than 64 blocks: sixteen waves have 24 tiles sooner than two launches (28 heads on 4,
+  // 760 tokens: 1 sequence 9.8 us against 10.1, 8 sequences 10.0 against 12.6, with masses 11.6 and 14.0, but 1 sequence with
+  // masses 11.4 against 10.6; 1000 tokens 9.9 against 9.3).  From 64 blocks on eight waves are one launch too, and sooner (64
+  // sequences 11.0 against 12.3, 200 29.7 against 41.1).
+  if (four && blocks < 64 && tiles > 16 && tiles <= 24) return {int(tiles), 1, 16};
   if (tiles <= (blocks >= 64 ? 32 : 16)) return {int(tiles), 1, tiles > 4 ? 8 : 4};
   const int64_t want = (std::min<int64_t>(2048, 512 * batch) + blocks - 1) / blocks;
   int64_t per = std::max<int64_t>(blocks <= 16 ? 4 : 8, (tiles + want - 1) / want);
