@@ -23,16 +23,17 @@
 // largest p.  Sums and statistics are float32.
 //
 // Caches of 4 bits are e2m1 codes with a power of two for each 32 dims: an
-// instruction widens two codes and applies the power, exactly.  16 sequences of
-// 65536 tokens of 4 heads of 128 in 107 us (5.1 TB/s); 24 of 28000 of 16 heads of 64 in
-// 170 us (4.3 TB/s).  On shorter ones, 24 of up to 6900 in 29 us (3.1 TB/s) and 5 for the join, start
-// and end weigh more; two tiles that share the columns of one softmax where query heads
+// instruction widens two codes and applies the power, exactly (past T's range: infinite).  16
+// sequences of 65536 tokens of 4 heads of 128 in 113 us (4.8 TB/s); 24 of 28000 of 16 heads of 64 in
+// 177 us with the join (4.1 TB/s).  On shorter ones, 24 of 6900 in 54 us (3.3 TB/s), start and end weigh
+// more, and where lengths differ (24 of up to 6900: 30 us and 5 for the join) runs cut by the longest leave
+// half of the blocks without tokens; two tiles that share the columns of one softmax where query heads
 // are few (a tenth fewer vector instructions) changed nothing.
 //
 // MASS: the kernel also leaves its scores, and what each token's weights come to
 // is added to its mass once the sums of all runs are known: by the same block
 // where it has all of them, else beside the join (131072 tokens of 28 heads on 4:
-// 7.7 us with the join, which is 5 alone).
+// 7.8 us with the join, which is 5 alone).
 #pragma once
 
 #include <algorithm>

@@ -6,7 +6,7 @@
 // of x / s rounded to nearest, ties to the even code; what lies beyond 6 s of the
 // largest power becomes that.  Every element is read once and written once, queries in
 // 16 bits, keys and values in 4.25; what bounds it are the vector instructions (6271
-// tokens of 32 + 2 x 32 heads of 64 in 28.6 us, 4.1 TB/s, 61 % of the SIMDs' cycles).
+// tokens of 32 + 2 x 32 heads of 64 in 27.7 us, 4.2 TB/s; they issue in 61 % of the cycles of busy compute units).
 //
 // Codes are those of the key rotated in float64: a float32 rotation would put
 // one code in 10^6 on the other side of a border (as a magnitude of 1.2 rounded to

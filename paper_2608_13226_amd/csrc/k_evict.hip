@@ -25,9 +25,9 @@
 //   evict_shift  the last rows, once the places at the front are empty
 //
 // Bound by the launches and barriers between dependent steps: 8 sequences of up to 1702
-// tokens of 4 heads, 64 of each out, 11.4 us; 131072 tokens of 4 heads halved 56 us
+// tokens of 4 heads, 64 of each out, 11.4 us; 131072 tokens of 4 heads halved 50 us
 // without the gaps between five launches, of which the rows, in scattered pieces of 64
-// and 4 bytes, take 17 to 24.
+// and 4 bytes, take 19.
 #include <algorithm>
 
 #include "launch.h"
